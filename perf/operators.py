@@ -1,0 +1,330 @@
+"""The work that the operators on token tables are measured on.
+
+A table holds one row per token: the embedding or the output matrix of a
+language model, or the codebook that k-means made its tokens with.  Four calls,
+as a program makes them:
+
+embed           the rows of the tokens, times a factor (first layer; decoding
+                of codes)
+embed_grad      its gradient: per token, the sum of the gradients of the
+                positions that hold it
+logprobs        scores of hidden rows against every row of the table, their
+                log-softmax at the given tokens, its entropy and log-sum-exp,
+                and the k best alternatives
+logprobs_grad   the gradient of the log probabilities (and, if asked for, of
+                the entropies) in the hidden rows and in the table
+
+Hidden rows and tables for the scores lie on a grid of sixteenths, as 8-bit
+quantised values do, and the scores' factor is a power of two: then every score
+is exact in 32 bits in any order of summation, and equal scores are real ties.
+A hidden row leans towards the row of one token, most often its target's, as a
+trained model's does.  Tokens follow a Zipf law over a shuffled vocabulary;
+some positions hold no token (-1).
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _embed(name, B, M, V, D, dtype):
+    return dict(name=name, op="embed", B=B, M=M, V=V, D=D, dtype=dtype, scale=math.sqrt(D))
+
+
+def _embed_grad(name, B, M, V, D, dtype, pad=0.0):
+    return dict(name=name, op="embed_grad", B=B, M=M, V=V, D=D, dtype=dtype, scale=math.sqrt(D), pad=pad)
+
+
+def _score_scale(D):
+    return 2.0 ** (1 - round(math.log2(math.sqrt(D))))
+
+
+def _logprobs(name, B, M, V, D, dtype, k=0, masked=0.0, pad=0.0):
+    return dict(name=name, op="logprobs", B=B, M=M, V=V, D=D, dtype=dtype, k=k, masked=masked,
+                pad=pad, scale=_score_scale(D))
+
+
+def _logprobs_grad(name, B, M, V, D, dtype, entropy=False, masked=0.0, pad=0.0):
+    return dict(name=name, op="logprobs_grad", B=B, M=M, V=V, D=D, dtype=dtype, entropy=entropy,
+                masked=masked, pad=pad, scale=_score_scale(D))
+
+
+def listed():
+    return [
+        # the token of one decoding step: a single row, latency alone
+        _embed("embed one token", 1, 1, 32_768, 1024, "bf16"),
+        # the prompts of a large batch
+        _embed("embed 16k tokens", 1, 16_384, 131_072, 4096, "bf16"),
+        # a small codebook in training, fp32, an odd number of positions
+        _embed_grad("embed grad codebook", 1, 4_099, 1024, 128, "f32"),
+        # a training batch over a large vocabulary, an eighth of it padding
+        _embed_grad("embed grad 32k tokens", 1, 32_768, 131_072, 2048, "bf16", pad=0.125),
+        # one decoding step with its alternatives
+        _logprobs("logprobs one token", 1, 1, 131_072, 4096, "bf16", k=20),
+        # a few sequences decoding, an odd vocabulary with forbidden tokens
+        _logprobs("logprobs 13 tokens", 1, 13, 50_021, 2048, "f16", k=5, masked=0.25),
+        # eight codebooks, each with its own hidden rows: units of quantised speech or images
+        _logprobs("logprobs 8 codebooks", 8, 4_096, 1_024, 128, "bf16"),
+        # prompts scored with alternatives
+        _logprobs("logprobs 4k prompt", 1, 4_096, 65_536, 1024, "bf16", k=20),
+        # the forward pass of a loss over a large vocabulary
+        _logprobs("logprobs 8k x 128k", 1, 8_192, 131_072, 4096, "bf16", pad=0.125),
+        # one codebook's classifier in training, odd sizes
+        _logprobs_grad("logprobs grad codebook", 1, 10_007, 1_003, 200, "f16"),
+        # eight codebooks in training
+        _logprobs_grad("logprobs grad 8 codebooks", 8, 4_096, 1_024, 128, "bf16", pad=0.125),
+        # the backward pass of a policy's loss with an entropy term
+        _logprobs_grad("logprobs grad 8k x 64k", 1, 8_192, 65_536, 2048, "bf16", entropy=True, pad=0.125),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(["embed", "embed_grad", "logprobs", "logprobs", "logprobs_grad", "logprobs_grad"])
+    B = 1 if rng.random() < 0.75 else rng.randint(2, 8)
+    while True:
+        D = _log(rng, 32, 4096)
+        D = D if rng.random() < 0.3 else max(32, D // 32 * 32)
+        V = _log(rng, 200, 131_072) // B + 1
+        M = _log(rng, 1, 16_384) // B + 1
+        if op == "embed":
+            c = _embed("", B, M, V, D, rng.choice(["f32", "bf16", "f16"]))
+        elif op == "embed_grad":
+            c = _embed_grad("", B, M, V, D, rng.choice(["f32", "bf16", "f16"]), rng.choice([0.0, 0.125]))
+        elif op == "logprobs":
+            k = rng.choice([0, 0, 1, 5, 8, 20, 32])
+            c = _logprobs("", B, M, V, D, rng.choice(["bf16", "bf16", "f16"]), k,
+                          rng.choice([0.0, 0.0, 0.25]), rng.choice([0.0, 0.125]))
+        else:
+            c = _logprobs_grad("", B, M, V, D, rng.choice(["bf16", "bf16", "f16"]), rng.random() < 0.4,
+                               rng.choice([0.0, 0.0, 0.25]), rng.choice([0.0, 0.125]))
+        del c["name"]
+        if B * V * D <= 131_072 * 2048 and (op.startswith("embed") or B * M * V * D <= 8_192 * 65_536 * 1024):
+            return c
+
+
+def _grid(shape, gen):
+    return (torch.randn(shape, device="cuda", generator=gen) * 16).round_().clamp_(-127, 127).div_(16)
+
+
+def _tokens(c, gen, pad):
+    """[B, M] tokens by a Zipf(1) law over a shuffled vocabulary; -1 where there is none."""
+    u = torch.rand((c["B"], c["M"]), device="cuda", generator=gen, dtype=torch.float64)
+    rank = (torch.exp(u * math.log(c["V"] + 1.0)) - 1).long().clamp_(0, c["V"] - 1)
+    t = torch.randperm(c["V"], device="cuda", generator=gen)[rank]
+    none = torch.rand((c["B"], c["M"]), device="cuda", generator=gen) < pad
+    return torch.where(none, -1, t).to(torch.int32)
+
+
+def prepare(case, seed):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    c, dt = case, DTYPES[case["dtype"]]
+    B, M, V, D = c["B"], c["M"], c["V"], c["D"]
+    s = {"op": c["op"], "scale": c["scale"], "V": V}
+    if c["op"] == "embed":
+        s["table"] = (torch.randn((B, V, D), device="cuda", generator=gen) / math.sqrt(D)).to(dt)
+        s["idx"] = _tokens(c, gen, 0.0)
+        return s
+    if c["op"] == "embed_grad":
+        s["grad"] = (torch.randn((B, M, D), device="cuda", generator=gen) * 1e-2).to(dt)
+        s["idx"] = _tokens(c, gen, c["pad"])
+        return s
+    W = _grid((B, V, D), gen)
+    s["target"] = _tokens(c, gen, c["pad"])
+    # the token that a row leans towards: its target, or in a third of the rows any other
+    other = torch.randint(0, V, (B, M), device="cuda", generator=gen)
+    use = (torch.rand((B, M), device="cuda", generator=gen) < 2 / 3) & (s["target"] >= 0)
+    lean = torch.where(use, s["target"].long(), other)
+    rows = torch.gather(W, 1, lean.unsqueeze(-1).expand(B, M, D))
+    X = torch.randn((B, M, D), device="cuda", generator=gen) + rows * (5 / math.sqrt(D))
+    s["X"] = (X * 16).round_().clamp_(-127, 127).div_(16).to(dt)
+    s["W"] = W.to(dt)
+    s["bias"] = None
+    if c["masked"]:  # tokens that are not allowed
+        off = torch.rand((B, V), device="cuda", generator=gen) < c["masked"]
+        s["bias"] = torch.where(off, float("-inf"), 0.0)
+    if c["op"] == "logprobs":
+        s["k"] = min(c["k"], V)
+        return s
+    # what the forward pass left, and the gradients that come back (of a loss that
+    # is scaled up, as 16-bit training does to keep small gradients in range)
+    _, s["entropy"], s["lse"], _, _ = _plain_logprobs(s["X"], s["W"], s["target"], 0, s["scale"], s["bias"])
+    up = 1024 / (B * M)
+    s["grad_logprob"] = torch.randn((B, M), device="cuda", generator=gen) * up
+    s["grad_entropy"] = torch.full((B, M), 0.01 * up, device="cuda") if c["entropy"] else None
+    if s["grad_entropy"] is None:
+        s["entropy"] = None
+    return s
+
+
+# ---------------------------------------------------------------------------
+# the plain forms, in 32 bits
+def _plain_scores(X, W, scale, bias):
+    z = torch.matmul(X.float(), W.float().transpose(1, 2)) * scale
+    return z if bias is None else z + bias.unsqueeze(1)
+
+
+def _plain_logprobs(X, W, target, k, scale, bias):
+    V = W.shape[1]
+    z = _plain_scores(X, W, scale, bias)
+    m = z.amax(-1, keepdim=True)
+    e = torch.exp(z - m)
+    total = e.sum(-1, keepdim=True)
+    lse = m + torch.log(total)
+    entropy = (lse - (torch.where(e > 0, z, 0.0) * e).sum(-1, keepdim=True) / total).squeeze(-1)
+    valid = (target >= 0) & (target < V)
+    at = torch.where(valid, target, 0).long().unsqueeze(-1)
+    logprob = torch.where(valid, (torch.gather(z, 2, at) - lse).squeeze(-1), 0.0)
+    top_idx = top_logprob = None
+    if k:  # the k best by (score, lower index): scores as ordered integers over the index
+        i = (z + 0.0).view(torch.int32)
+        key = ((i ^ ((i >> 31) & 0x7FFFFFFF)).long() << 32) + (V - 1 - torch.arange(V, device=z.device))
+        best = torch.topk(key, k, dim=-1, sorted=True).values
+        top = V - 1 - (best & 0xFFFFFFFF)
+        v = torch.gather(z, 2, top)
+        top_logprob = v - lse
+        top_idx = torch.where(v == float("-inf"), -1, top).to(torch.int32)
+    return logprob, entropy, lse.squeeze(-1), top_idx, top_logprob
+
+
+def _plain_logprobs_grad(X, W, target, lse, grad_logprob, entropy, grad_entropy, scale, bias):
+    V = W.shape[1]
+    z = _plain_scores(X, W, scale, bias)
+    p = torch.exp(z - lse.unsqueeze(-1))
+    valid = (target >= 0) & (target < V)
+    at = torch.where(valid, target, 0).long().unsqueeze(-1)
+    # a masked target's log probability is -inf whatever the inputs: no gradient
+    g = torch.where(valid & (torch.gather(z, 2, at).squeeze(-1) > float("-inf")), grad_logprob, 0.0).unsqueeze(-1)
+    dz = -g * p
+    if grad_entropy is not None:
+        logp = torch.where(p > 0, z - lse.unsqueeze(-1), 0.0)
+        dz -= grad_entropy.unsqueeze(-1) * p * (logp + entropy.unsqueeze(-1))
+    dz.scatter_add_(2, at, g)
+    dz *= scale
+    dX = torch.matmul(dz, W.float())
+    dW = torch.matmul(dz.transpose(1, 2).contiguous(), X.float())
+    return dX.to(X.dtype), dW.to(W.dtype)
+
+
+def _plain_embed(table, idx, scale):
+    valid = (idx >= 0) & (idx < table.shape[1])
+    at = torch.where(valid, idx, 0).long().unsqueeze(-1)
+    rows = torch.gather(table, 1, at.expand(-1, -1, table.shape[2])).float() * scale
+    return torch.where(valid.unsqueeze(-1), rows, 0.0).to(table.dtype)
+
+
+def _plain_embed_grad(grad, idx, V, scale):
+    B, M, D = grad.shape
+    valid = (idx >= 0) & (idx < V)
+    at = torch.where(valid, idx, 0).long() + torch.arange(B, device=idx.device).unsqueeze(1) * V
+    g = torch.where(valid.unsqueeze(-1), grad.float(), 0.0).reshape(B * M, D)
+    out = torch.zeros((B * V, D), device=grad.device).index_add_(0, at.reshape(-1), g)
+    return (out * scale).to(grad.dtype).view(B, V, D)
+
+
+def run(state):
+    s = state
+    if own:
+        from paper_2608_12629_amd import kmeans
+    if s["op"] == "embed":
+        if own:
+            return kmeans.kmeans_embed(s["table"], s["idx"], s["scale"])
+        return _plain_embed(s["table"], s["idx"], s["scale"])
+    if s["op"] == "embed_grad":
+        if own:
+            return kmeans.kmeans_embed_grad(s["grad"], s["idx"], s["V"], s["scale"])
+        return _plain_embed_grad(s["grad"], s["idx"], s["V"], s["scale"])
+    if s["op"] == "logprobs":
+        if own:
+            r = kmeans.kmeans_logprobs(s["X"], s["W"], s["target"], k=s["k"], scale=s["scale"], bias=s["bias"])
+        else:
+            r = _plain_logprobs(s["X"], s["W"], s["target"], s["k"], s["scale"], s["bias"])
+        return list(r) if s["k"] else list(r[:3])
+    if own:
+        return list(kmeans.kmeans_logprobs_grad(
+            s["X"], s["W"], s["target"], s["lse"], s["grad_logprob"], entropy=s["entropy"],
+            grad_entropy=s["grad_entropy"], scale=s["scale"], bias=s["bias"]))
+    return list(_plain_logprobs_grad(s["X"], s["W"], s["target"], s["lse"], s["grad_logprob"], s["entropy"],
+                                     s["grad_entropy"], s["scale"], s["bias"]))
+
+
+def work(case):
+    c = case
+    e = 4 if c["dtype"] == "f32" else 2
+    B, M, V, D = c["B"], c["M"], c["V"], c["D"]
+    rows, table = M * D * e, V * D * e
+    if c["op"] == "embed":  # each row of the table once at most
+        return {"bytes": B * (rows + min(rows, table) + 4 * M), "flops": B * M * D}
+    if c["op"] == "embed_grad":
+        return {"bytes": B * (rows + table + 4 * M), "flops": B * M * D}
+    bias = 4 * V if c["masked"] else 0
+    if c["op"] == "logprobs":
+        return {"bytes": B * (rows + table + bias + M * (16 + 8 * c["k"])), "flops": 2 * B * M * V * D}
+    return {"bytes": B * (2 * rows + 2 * table + bias + M * (20 if c["entropy"] else 12)), "flops": 6 * B * M * V * D}
+
+
+# ---------------------------------------------------------------------------
+def exact(case, seed):
+    """The definitions in 64 bits, instance by instance and in blocks of rows."""
+    s = prepare(case, seed)
+    V, scale = s["V"], s["scale"]
+    inf = float("inf")
+    if s["op"] == "embed":
+        table, idx = s["table"].double(), s["idx"].long()
+        out = torch.zeros((*idx.shape, table.shape[2]), dtype=torch.float64, device="cuda")
+        for b in range(idx.shape[0]):
+            ok = ((idx[b] >= 0) & (idx[b] < V)).nonzero().squeeze(1)
+            out[b, ok] = table[b, idx[b, ok]] * scale
+        return out
+    if s["op"] == "embed_grad":
+        grad, idx = s["grad"], s["idx"].long()
+        out = torch.zeros((idx.shape[0], V, grad.shape[2]), dtype=torch.float64, device="cuda")
+        for b in range(idx.shape[0]):
+            ok = ((idx[b] >= 0) & (idx[b] < V)).nonzero().squeeze(1)
+            order = ok[torch.sort(idx[b, ok], stable=True).indices]
+            tok, counts = torch.unique_consecutive(idx[b, order], return_counts=True)
+            total = torch.cumsum(grad[b, order].double(), 0)[torch.cumsum(counts, 0) - 1]
+            out[b, tok] = torch.diff(total, dim=0, prepend=torch.zeros_like(total[:1])) * scale
+        return out
+    outs = []
+    for b in range(s["X"].shape[0]):
+        X, Wt = s["X"][b].double(), s["W"][b].double().t().contiguous()
+        got = []
+        if s["op"] == "logprobs_grad":
+            dW = torch.zeros((V, X.shape[1]), dtype=torch.float64, device="cuda")
+        for r0 in range(0, X.shape[0], 2048):
+            x, t = X[r0:r0 + 2048], s["target"][b, r0:r0 + 2048].long()
+            z = x.mm(Wt).mul_(scale)
+            if s["bias"] is not None:
+                z += s["bias"][b].double()
+            lse = torch.logsumexp(z, 1)
+            p = (z - lse[:, None]).exp_()
+            ent = -torch.special.xlogy(p, p).sum(1)
+            has = (t >= 0) & (t < V)
+            zt = z[torch.arange(len(t), device="cuda"), t.clamp(0, V - 1)]
+            if s["op"] == "logprobs":
+                part = [torch.where(has, zt - lse, 0), ent, lse]
+                if s["k"]:
+                    part.append(z.topk(s["k"], 1).values - lse[:, None])
+            else:
+                g = torch.where(has & (zt > -inf), s["grad_logprob"][b, r0:r0 + 2048].double(), 0)
+                if s["grad_entropy"] is not None:
+                    ge = s["grad_entropy"][b, r0:r0 + 2048].double()[:, None]
+                    dz = -p * g[:, None] - ge * (torch.special.xlogy(p, p) + p * ent[:, None])
+                else:
+                    dz = -p * g[:, None]
+                dz[torch.arange(len(t), device="cuda"), t.clamp(0, V - 1)] += g
+                part = [dz.mm(Wt.t().contiguous()) * scale]
+                dW += dz.t().contiguous().mm(x) * scale
+            got.append(part)
+        part = [torch.cat(p) for p in zip(*got)]
+        outs.append(part if s["op"] == "logprobs" else [*part, dW])
+    outs = [torch.stack(p) for p in zip(*outs)]
+    return [*outs[:3], None, *outs[3:]] if s["op"] == "logprobs" and s["k"] else outs
