@@ -232,23 +232,23 @@ def _plain_embed_grad(grad, idx, V, scale):
 def run(state):
     s = state
     if own:
-        from paper_2608_12629_amd import kmeans
+        from paper_2608_12629_amd import tokens
     if s["op"] == "embed":
         if own:
-            return kmeans.kmeans_embed(s["table"], s["idx"], s["scale"])
+            return tokens.tokens_embed(s["table"], s["idx"], s["scale"])
         return _plain_embed(s["table"], s["idx"], s["scale"])
     if s["op"] == "embed_grad":
         if own:
-            return kmeans.kmeans_embed_grad(s["grad"], s["idx"], s["V"], s["scale"])
+            return tokens.tokens_embed_grad(s["grad"], s["idx"], s["V"], s["scale"])
         return _plain_embed_grad(s["grad"], s["idx"], s["V"], s["scale"])
     if s["op"] == "logprobs":
         if own:
-            r = kmeans.kmeans_logprobs(s["X"], s["W"], s["target"], k=s["k"], scale=s["scale"], bias=s["bias"])
+            r = tokens.tokens_logprobs(s["X"], s["W"], s["target"], k=s["k"], scale=s["scale"], bias=s["bias"])
         else:
             r = _plain_logprobs(s["X"], s["W"], s["target"], s["k"], s["scale"], s["bias"])
         return list(r) if s["k"] else list(r[:3])
     if own:
-        return list(kmeans.kmeans_logprobs_grad(
+        return list(tokens.tokens_logprobs_grad(
             s["X"], s["W"], s["target"], s["lse"], s["grad_logprob"], entropy=s["entropy"],
             grad_entropy=s["grad_entropy"], scale=s["scale"], bias=s["bias"]))
     return list(_plain_logprobs_grad(s["X"], s["W"], s["target"], s["lse"], s["grad_logprob"], s["entropy"],
