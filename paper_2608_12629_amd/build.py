@@ -17,7 +17,8 @@ CALIB_LIB = os.path.join(HERE, "libfkm_calib.so")
 CALIB_SOURCES = ["calib.hip"]
 SOURCES = ["api.hip", "assign.hip", "assign_pipe_bf16.hip", "assign_pipe_f16.hip",
            "assign_smallk_bf16.hip", "assign_smallk_f16.hip", "assign_tiled.hip", "update.hip",
-           "knn_bf16.hip", "knn_f16.hip", "knn_scan_bf16.hip", "knn_scan_f16.hip"]
+           "knn_bf16.hip", "knn_f16.hip", "knn_scan_bf16.hip", "knn_scan_f16.hip", "tokens_api.hip", "tokens_embed.hip",
+           "logprobs_bf16.hip", "logprobs_f16.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -10,6 +10,7 @@
 
 #include "../../include/flashkmeans.h"
 #include "fkm_internal.h"
+#include "tokens_internal.h"
 
 namespace fkm {
 
@@ -114,7 +115,7 @@ static hipError_t pad_inputs(const void* X, const float* C, int dt, const Worksp
   return e;
 }
 
-static int check_ptrs(std::initializer_list<const void*> ps) {
+int check_ptrs(std::initializer_list<const void*> ps) {
   for (const void* p : ps)
     if (!p || !aligned16(p)) return FKM_ERR_INVALID_ARG;
   return FKM_OK;
@@ -130,7 +131,7 @@ static int check_ws(void* ws, size_t ws_bytes, int64_t B, int64_t N, int64_t D, 
 // 0 = not checked yet, 1 = gfx950, 2 = other device
 static std::atomic<int> g_arch[256];
 
-static int check_device() {
+int check_device() {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess) return FKM_ERR_HIP;
   if (dev < 0 || dev >= 256) return FKM_ERR_UNSUPPORTED;
@@ -145,7 +146,7 @@ static int check_device() {
   return st == 1 ? FKM_OK : FKM_ERR_UNSUPPORTED;
 }
 
-static int hip_status(hipError_t e) { return e == hipSuccess ? FKM_OK : FKM_ERR_HIP; }
+int hip_status(hipError_t e) { return e == hipSuccess ? FKM_OK : FKM_ERR_HIP; }
 
 // The workspace of kmeans_lloyd_noalloc: a static device array, one per GPU,
 // alive until the process ends.  In host code `scratch` names a host-side

@@ -1,0 +1,1038 @@
+// logprobs.h -- scores of rows against a whole token table and what follows from
+// them (include/flashtokens.h): log-softmax, entropy, the best alternatives, and
+// the gradients.  Instantiated per storage type in logprobs_bf16.hip and
+// logprobs_f16.hip.
+//
+// One tiled product carries it all, P[a, b] = sum_c A[a, c] B[b, c] with both
+// operands' contraction contiguous: 256 (or 128) rows of A by 256 rows of B to a
+// workgroup of eight waves, each 2 (or 1) x 4 tiles of 32 x 32 x 16 MFMAs.  Stages of
+// 32 elements of both operands go from L2 straight into one of four LDS buffers,
+// two to three stages ahead of the MFMAs, which read them conflict-free from
+// swizzled rows.  A's rows lie in a lane's registers and B's across the lanes, so
+// with the table as A a lane holds 32 scores of one position and the softmax's
+// running maximum, sum and weighted sum stay in that lane until the last block.
+#pragma once
+
+#include <algorithm>
+
+#include "fkm_device.h"
+#include "tokens_internal.h"
+
+namespace fkm {
+
+namespace {
+
+constexpr int NT_T = 512;  // threads of a workgroup
+constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float NEG_INF = -__builtin_inff();
+
+__device__ const uint4 nt_zero = {0, 0, 0, 0};
+
+// L2 -> LDS copies of 16 (or 4) bytes a lane into the wave's slots at `lds`, issued
+// by inline assembly so that only the explicit waits below govern them; M0 (the LDS
+// base) is set in the same statement, one wait state before the load reads it.
+__device__ __forceinline__ void nt_dma16(const void* src, char* lds) {
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(src), "s"(base)
+               : "memory");
+}
+__device__ __forceinline__ void nt_dma4(const void* src, char* lds) {
+  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+               :
+               : "v"(src), "s"(base)
+               : "memory");
+}
+
+// Until at most n of this wave's vector memory operations are in flight and its LDS
+// reads are done, then a barrier that leaves the later loads in flight.
+template <int n>
+__device__ __forceinline__ void nt_wait_and_sync() {
+  __builtin_amdgcn_s_waitcnt((n & 0xF) | ((n >> 4) << 14) | (7 << 4));
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// Row r of a stage keeps its four 16-byte chunks in slots c ^ swz(r).
+__device__ __forceinline__ int nt_swz(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
+
+template <typename T>
+__device__ __forceinline__ T& nt_at(char* base, int off) {
+  return *reinterpret_cast<T*>(base + off);
+}
+
+template <int TCW, bool BIAS>
+struct NtSize {
+  static constexpr int BA = 128 * TCW;           // rows of A in a block
+  static constexpr int AB = BA * 64;             // bytes of A in a stage
+  static constexpr int BBY = LP_BB * 64;         // bytes of B
+  static constexpr int STAGE = AB + BBY + (BIAS ? NT_T * 4 : 0);
+  static constexpr int LOADS = TCW + 2 + (BIAS ? 1 : 0);  // loads of a thread in a stage
+  static constexpr int SMEM = 4 * STAGE;
+};
+
+// The operands of a workgroup: rows a0 .. of A (nblk blocks) by rows b0 .. of B,
+// chunks [c0, c1) of the contraction.  Rows past the last one are read as the last
+// one (their results are dropped), chunks past c1 as zeros.
+struct NtIn {
+  const char *A, *B;
+  const float* bias;  // of A's rows
+  int64_t lda, ldb;   // bytes of a row
+  int nA, nB, a0, b0, c0, c1, nblk;
+};
+
+template <int TCW>
+struct NtFrag {
+  uint4 a[TCW], b[4];
+};
+
+template <int DT, int TCW, bool BIAS>
+struct NtLoop {
+  using Z = NtSize<TCW, BIAS>;
+  const char *ap[TCW], *bp[2];
+  const float* biasp;
+  NtIn in;
+  int tid, wave, cc, iblk, id, nds;  // the stage to load next: block iblk, stage id of it
+  int loff0, loff1, wp, wc;
+  char* smem;
+
+  __device__ __forceinline__ void block_rows(int blk) {
+    const int r = in.a0 + blk * Z::BA + (tid >> 2);
+#pragma unroll
+    for (int u = 0; u < TCW; ++u)
+      ap[u] = in.A + (int64_t)min(r + 128 * u, in.nA - 1) * in.lda + (in.c0 + cc) * 16;
+    if constexpr (BIAS)
+      biasp = in.bias + min(in.a0 + blk * Z::BA + (tid & (Z::BA - 1)), in.nA - 1);
+  }
+
+  __device__ __forceinline__ void init(const NtIn& i, char* sm) {
+    in = i;
+    smem = sm;
+    tid = threadIdx.x;
+    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lane = tid & 63, n = lane & 31, h = lane >> 5;
+    cc = (tid & 3) ^ nt_swz(tid >> 2);
+    nds = (in.c1 - in.c0 + 3) / 4;
+    iblk = id = 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      bp[u] = in.B + (int64_t)min(in.b0 + (tid >> 2) + 128 * u, in.nB - 1) * in.ldb + (in.c0 + cc) * 16;
+    block_rows(0);
+    // lane 32 h + n reads row (tile base + n), chunk 2 step + h
+    loff0 = n * 64 + ((0 + h) ^ nt_swz(n)) * 16;
+    loff1 = n * 64 + ((2 + h) ^ nt_swz(n)) * 16;
+    wp = wave & 1;   // half of B's rows
+    wc = wave >> 1;  // quarter of A's rows
+  }
+
+  __device__ __forceinline__ void issue(char* buf) {
+    const bool in_range = in.c0 + id * 4 + cc < in.c1;
+    const int off = id * 64;
+#pragma unroll
+    for (int u = 0; u < TCW; ++u)
+      nt_dma16(in_range ? ap[u] + off : (const char*)&nt_zero, buf + (u * NT_T + wave * 64) * 16);
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      nt_dma16(in_range ? bp[u] + off : (const char*)&nt_zero,
+               buf + Z::AB + (u * NT_T + wave * 64) * 16);
+    if constexpr (BIAS) nt_dma4(biasp, buf + Z::AB + Z::BBY + wave * 256);
+    if (++id == nds) {
+      id = 0;
+      block_rows(++iblk);
+    }
+  }
+
+  __device__ __forceinline__ void read(NtFrag<TCW>& f, char* buf, int lo) {
+#pragma unroll
+    for (int tc = 0; tc < TCW; ++tc) f.a[tc] = nt_at<uint4>(buf, (wc * TCW + tc) * 2048 + lo);
+#pragma unroll
+    for (int tp = 0; tp < 4; ++tp)
+      f.b[tp] = nt_at<uint4>(buf, Z::AB + (wp * 4 + tp) * 2048 + lo);
+  }
+
+  __device__ __forceinline__ void mfma(f32x16 (&acc)[4][TCW], const NtFrag<TCW>& f) {
+#pragma unroll
+    for (int tp = 0; tp < 4; ++tp)
+#pragma unroll
+      for (int tc = 0; tc < TCW; ++tc) acc[tp][tc] = mfma32_chunk<DT>(f.a[tc], f.b[tp], acc[tp][tc]);
+  }
+
+  // epi(acc, block, bias of the block in LDS) after each block
+  template <class Epi>
+  __device__ __forceinline__ void run(Epi&& epi) {
+    const int S = in.nblk * nds;
+    auto buf = [&](int s) { return smem + (s & 3) * Z::STAGE; };
+    issue(buf(0));
+    if (1 < S) issue(buf(1));
+    if (2 < S) issue(buf(2));
+    if (2 < S) nt_wait_and_sync<2 * Z::LOADS>();
+    else if (1 < S) nt_wait_and_sync<Z::LOADS>();
+    else nt_wait_and_sync<0>();
+    NtFrag<TCW> f0, f1;
+    read(f0, buf(0), loff0);
+    f32x16 acc[4][TCW];
+    int s = 0;
+    for (int g = 0; g < in.nblk; ++g) {
+#pragma unroll
+      for (int tp = 0; tp < 4; ++tp)
+#pragma unroll
+        for (int tc = 0; tc < TCW; ++tc)
+#pragma unroll
+          for (int j = 0; j < 16; ++j) acc[tp][tc][j] = 0.f;
+      for (int d = 0; d < nds; ++d, ++s) {
+        // stage s: its second step's fragments, the first step's MFMAs, then wait for
+        // stage s + 1, start stage s + 3 into the buffer of stage s - 1 (which every
+        // wave has finished), read stage s + 1's first fragments
+        read(f1, buf(s), loff1);
+        mfma(acc, f0);
+        // (vmcnt counts in issue order: an epilogue's stores only make the wait longer)
+        if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
+        else nt_wait_and_sync<0>();
+        if (s + 3 < S) issue(buf(s + 3));
+        if (s + 1 < S) read(f0, buf(s + 1), loff0);
+        mfma(acc, f1);
+      }
+      epi(acc, g, reinterpret_cast<const float*>(buf(s - 1) + Z::AB + Z::BBY));
+    }
+  }
+};
+
+// ---- softmax statistics ----------------------------------------------------------
+// Of some scores z: m = max (at least -FLT_MAX), s = sum exp(z - m), t = sum
+// exp(z - m) (z - m).  -inf scores add nothing.
+struct Stat {
+  float m, s, t;
+};
+__device__ __forceinline__ Stat stat_none() { return {-__FLT_MAX__, 0.f, 0.f}; }
+// The same about a larger maximum m.
+__device__ __forceinline__ void stat_raise(Stat& a, float m) {
+  const float d = __builtin_fmaxf(a.m - m, -1e30f);
+  const float f = __builtin_amdgcn_exp2f(d * LOG2E);
+  a.t = f * __builtin_fmaf(d, a.s, a.t);
+  a.s *= f;
+  a.m = m;
+}
+__device__ __forceinline__ Stat stat_merge(Stat a, Stat b) {
+  const float m = __builtin_fmaxf(a.m, b.m);
+  stat_raise(a, m);
+  stat_raise(b, m);
+  return {m, a.s + b.s, a.t + b.t};
+}
+
+// ---- scores --------------------------------------------------------------------
+// One workgroup: 256 rows of X by a share of the column blocks.  Share sp of the columns and
+// row block mb are chosen so that the workgroups of an XCD (ids go round-robin over
+// the eight) share a few column shares and row blocks through its L2.
+struct ScoreGrid {
+  int nmb, splits;  // row blocks, shares of the column blocks (all within one of a size)
+};
+__device__ __forceinline__ bool score_place(const ScoreGrid& g, int id, int& mb, int& sp) {
+  if (g.splits >= 8) {  // shares dealt to the XCDs; 8 row blocks at a time, shares inside
+    const int xcd = id & 7, j = id >> 3, sx = (g.splits + 7) / 8;
+    const int gm = min(8, g.nmb), sup = j / (gm * sx), r = j % (gm * sx);
+    mb = sup * gm + r % gm;
+    sp = xcd * sx + r / gm;
+    return mb < g.nmb && sp < g.splits;
+  }
+  sp = id % g.splits;
+  mb = id / g.splits;
+  return mb < g.nmb;
+}
+inline unsigned score_blocks(const ScoreGrid& g) {
+  if (g.splits < 8) return (unsigned)(g.nmb * g.splits);
+  const int sx = (g.splits + 7) / 8, gm = std::min(8, g.nmb);
+  return (unsigned)((g.nmb + gm - 1) / gm * gm * sx * 8);
+}
+
+struct ScoreArgs {
+  const char *X, *W;
+  const float* bias;
+  const int32_t* target;
+  int64_t xs, ws, ts;    // instance strides: bytes, bytes, positions
+  int64_t rows;          // rows of this block of rows
+  int64_t ld;            // bytes of a row
+  int V, chunks;         // 16-byte chunks of a row
+  float scale;
+  ScoreGrid grid;
+  float4* part;          // [B, splits, rows]
+  float* zt;             // [B, rows]
+  float *z, *gmax;       // [B, rows, ldz], [B, rows, groups]
+  int64_t ldz, groups;
+};
+
+template <int DT, bool BIAS, bool TOPK>
+__global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
+  using Z = NtSize<2, BIAS>;
+  __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
+  int mb, sp;
+  if (!score_place(a.grid, blockIdx.x, mb, sp)) return;
+  const int64_t b = blockIdx.y;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  const int64_t nvb = (a.V + 255) / 256;
+  const int blk0 = (int)(nvb * sp / a.grid.splits), blk1 = (int)(nvb * (sp + 1) / a.grid.splits);
+  NtIn in;
+  in.A = a.W + b * a.ws;
+  in.B = a.X + b * a.xs;
+  in.bias = BIAS ? a.bias + b * a.V : nullptr;
+  in.lda = in.ldb = a.ld;
+  in.nA = a.V;
+  in.nB = (int)a.rows;
+  in.a0 = blk0 * 256;
+  in.b0 = mb * LP_BB;
+  in.c0 = 0;
+  in.c1 = a.chunks;
+  in.nblk = blk1 - blk0;
+  NtLoop<DT, 2, BIAS> loop;
+  loop.init(in, smem);
+  const int wp = loop.wp, wc = loop.wc;
+  Stat st[4];
+  float zt[4];
+  int tgt[4];
+#pragma unroll
+  for (int tp = 0; tp < 4; ++tp) {
+    const int r = in.b0 + wp * 128 + tp * 32 + n;
+    st[tp] = stat_none();
+    zt[tp] = 0.f;
+    tgt[tp] = a.target && r < a.rows ? a.target[b * a.ts + r] : -1;
+  }
+  auto epi = [&](f32x16(&acc)[4][2], int g, const float* bias) {
+    const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
+    const bool edge = v0 + 64 > a.V;
+    float bz[2][16];
+    if constexpr (BIAS) {
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) bz[tc][4 * q + r] = x[r];
+        }
+    }
+#pragma unroll
+    for (int tp = 0; tp < 4; ++tp) {
+      float z[2][16], lm = -__FLT_MAX__;
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          float x;
+          if constexpr (BIAS)  // a forbidden token's score is -inf, whatever its row holds
+            x = bz[tc][j] == NEG_INF ? NEG_INF : __builtin_fmaf(acc[tp][tc][j], a.scale, bz[tc][j]);
+          else
+            x = acc[tp][tc][j] * a.scale;
+          z[tc][j] = x;
+        }
+      if (edge) {
+#pragma unroll
+        for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (v0 + tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3) >= a.V) z[tc][j] = NEG_INF;
+      }
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) lm = __builtin_fmaxf(lm, z[tc][j]);
+      if (lm > st[tp].m) stat_raise(st[tp], lm);
+      float es = 0.f, et = 0.f;
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const float u = z[tc][j] - st[tp].m;
+          const float e = __builtin_amdgcn_exp2f(u * LOG2E);
+          es += e;
+          et = __builtin_fmaf(e, __builtin_fmaxf(u, -1e30f), et);  // 0 for -inf
+        }
+      st[tp].s += es;
+      st[tp].t += et;
+      // the target, if it is among this lane's 32 columns
+      const int rel = tgt[tp] - v0;
+      const bool hit = (unsigned)rel < 64u && ((rel >> 2) & 1) == h;
+      if (__ballot(hit)) {
+#pragma unroll
+        for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+          for (int j = 0; j < 16; ++j)
+            if (hit && rel == tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3)) zt[tp] = z[tc][j];
+      }
+      if constexpr (TOPK) {
+        const int64_t row = in.b0 + wp * 128 + tp * 32 + n;
+        const float gm = __builtin_fmaxf(lm, __shfl_xor(lm, 32));
+        if (row < a.rows) {
+          if (h == 0) a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = gm;
+          float* zr = a.z + (b * a.rows + row) * a.ldz + v0 + 4 * h;
+#pragma unroll
+          for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+              *reinterpret_cast<f32x4*>(zr + tc * 32 + 8 * q) =
+                  f32x4{z[tc][4 * q], z[tc][4 * q + 1], z[tc][4 * q + 2], z[tc][4 * q + 3]};
+        }
+      }
+    }
+  };
+  loop.run(epi);
+
+  // the two lanes of a row, then the four waves that share it, in a fixed order
+  __syncthreads();
+  Stat* sh = reinterpret_cast<Stat*>(smem);  // [4][256]
+#pragma unroll
+  for (int tp = 0; tp < 4; ++tp) {
+    const int rl = wp * 128 + tp * 32 + n, rel = tgt[tp] - in.a0;
+    // the score of a target among this share's columns, from the lane that held it
+    if ((unsigned)tgt[tp] < (unsigned)a.V && (unsigned)rel < (unsigned)(in.nblk * 256) &&
+        ((rel >> 2) & 1) == h && ((rel >> 6) & 3) == wc)
+      a.zt[b * a.rows + in.b0 + rl] = zt[tp];
+    Stat o = {__shfl_xor(st[tp].m, 32), __shfl_xor(st[tp].s, 32), __shfl_xor(st[tp].t, 32)};
+    o = stat_merge(h ? o : st[tp], h ? st[tp] : o);
+    if (h == 0) sh[wc * LP_BB + rl] = o;
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < LP_BB; r += NT_T) {
+    Stat o = sh[r];
+#pragma unroll
+    for (int q = 1; q < 4; ++q) o = stat_merge(o, sh[q * LP_BB + r]);
+    if (in.b0 + r < a.rows)
+      a.part[(b * a.grid.splits + sp) * a.rows + in.b0 + r] = make_float4(o.m, o.s, o.t, 0.f);
+  }
+}
+
+// Scores as integers in the same order (-0 as +0).
+__device__ __forceinline__ uint32_t score_key(float v) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
+}
+__device__ __forceinline__ float key_score(uint32_t u) {
+  return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
+}
+
+struct FinishArgs {
+  const float4* part;
+  const float* zt;
+  const float *z, *gmax;
+  const int32_t* target;
+  int64_t rows, ts, ldz, groups;
+  int splits, V, k;
+  float *logprob, *entropy, *lse;  // of this block of rows; ts positions an instance
+  int32_t* top_idx;
+  float* top_logprob;
+};
+
+// One wave per row: the shares' statistics merged, and the k best: the k groups of
+// the largest best scores (ties to the lowest group) hold them, since each of these
+// has an entry as good as anything elsewhere; then k times the best of their entries.
+template <bool TOPK>
+__global__ __launch_bounds__(64) void logprobs_finish_kernel(FinishArgs a) {
+  const int64_t row = blockIdx.x, b = blockIdx.y;
+  const int lane = threadIdx.x;
+  Stat st = stat_none();
+  for (int sp = lane; sp < a.splits; sp += 64) {
+    const float4 p = a.part[(b * a.splits + sp) * a.rows + row];
+    st = stat_merge(st, Stat{p.x, p.y, p.z});
+  }
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) {
+    const Stat o = {__shfl_xor(st.m, m), __shfl_xor(st.s, m), __shfl_xor(st.t, m)};
+    st = stat_merge(lane & m ? o : st, lane & m ? st : o);
+  }
+  const bool none = st.s == 0.f;  // every token is forbidden
+  const float logs = logf(st.s), lse = none ? NEG_INF : st.m + logs;
+  if (lane == 0) {
+    const int64_t o = b * a.ts + row;
+    a.lse[o] = lse;
+    if (a.entropy) a.entropy[o] = none ? 0.f : logs - st.t / st.s;
+    if (a.target) {
+      const int t = a.target[o];
+      a.logprob[o] = (unsigned)t >= (unsigned)a.V ? 0.f
+                     : none ? NEG_INF : (a.zt[b * a.rows + row] - st.m) - logs;
+    }
+  }
+  if constexpr (TOPK) {
+    extern __shared__ uint32_t gk[];  // keys of the groups' best scores
+    __shared__ int sel[TOK_MAX_K];
+    const float* gm = a.gmax + (b * a.rows + row) * a.groups;
+    const int G = (int)a.groups, k = a.k, kg = min(k, G);
+    for (int i = lane; i < G; i += 64) gk[i] = score_key(gm[i]);
+    __syncthreads();
+    uint32_t kth = 0;  // the kg-th largest: the largest value that kg groups reach
+    for (int bit = 31; bit >= 0; --bit) {
+      const uint32_t c = kth | (1u << bit);
+      int cnt = 0;
+      for (int i = lane; i < G; i += 64) cnt += gk[i] >= c ? 1 : 0;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) cnt += __shfl_xor(cnt, m);
+      if (cnt >= kg) kth = c;
+    }
+    int above = 0;
+    for (int i = lane; i < G; i += 64) above += gk[i] > kth ? 1 : 0;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) above += __shfl_xor(above, m);
+    int ties = kg - above, got = 0;  // groups at kth itself to take, lowest first
+    for (int i0 = 0; i0 < G && got < kg; i0 += 64) {
+      const int i = i0 + lane;
+      const uint32_t key = i < G ? gk[i] : 0u;
+      const bool over = i < G && key > kth, tie = i < G && key == kth;
+      const uint64_t tm = __ballot(tie);
+      const uint64_t below = (1ull << lane) - 1;
+      const bool take = over || (tie && __popcll(tm & below) < ties);
+      const uint64_t km = __ballot(take);
+      if (take) sel[got + __popcll(km & below)] = i;
+      got += __popcll(km);
+      ties -= min(ties, (int)__popcll(tm));
+    }
+    __syncthreads();
+    // entry `lane` of each chosen group; groups in ascending order
+    const float* zr = a.z + (b * a.rows + row) * a.ldz;
+    uint32_t key[TOK_MAX_K];
+#pragma unroll
+    for (int i = 0; i < TOK_MAX_K; ++i)
+      key[i] = i < kg ? score_key(zr[(int64_t)sel[i] * LP_GROUP + lane]) : 0u;
+    for (int j = 0; j < k; ++j) {
+      uint32_t best = 0;
+      int at = -1;
+#pragma unroll
+      for (int i = 0; i < TOK_MAX_K; ++i)
+        if (key[i] > best) best = key[i], at = i;
+      int v = at >= 0 ? sel[at] * LP_GROUP + lane : 0x7fffffff;
+      uint32_t wb = best;
+      int wv = v;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) {
+        const uint32_t ob = __shfl_xor(wb, m);
+        const int ov = __shfl_xor(wv, m);
+        if (ob > wb || (ob == wb && ov < wv)) wb = ob, wv = ov;
+      }
+      if (at >= 0 && v == wv) {
+#pragma unroll
+        for (int i = 0; i < TOK_MAX_K; ++i)
+          if (i == at) key[i] = 0u;
+      }
+      if (lane == 0) {
+        const float zb = key_score(wb);
+        const bool have = wb > score_key(NEG_INF) && wv < a.V && !none;
+        const int64_t o = (b * a.ts + row) * k + j;
+        a.top_idx[o] = have ? wv : -1;
+        a.top_logprob[o] = have ? (zb - st.m) - logs : NEG_INF;
+      }
+    }
+  }
+}
+
+// ---- gradient ------------------------------------------------------------------
+constexpr float F16_UP = 2048.f;  // dz of fp16 rows is stored this much larger
+
+// What each position's gradient needs.  fp16: dz is stored over the power of two gs at
+// or above max(|g|, |h|), so that small probabilities stay in range.
+template <int DT>
+__global__ __launch_bounds__(256) void grad_rows_kernel(
+    const int32_t* __restrict__ target, const float* __restrict__ lse,
+    const float* __restrict__ ent, const float* __restrict__ g, const float* __restrict__ h,
+    const float* __restrict__ bias, int64_t rows, int64_t M, int V, RowGrad* __restrict__ out) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += (int64_t)gridDim.x * 256) {
+    RowGrad r;
+    const int t = target[i];
+    r.target = (unsigned)t < (unsigned)V && (!bias || bias[(i / M) * V + t] != NEG_INF) ? t : -1;
+    r.lse = lse[i];
+    const bool any = r.lse != NEG_INF;
+    r.g = r.target >= 0 ? g[i] : 0.f;
+    r.h = h ? h[i] : 0.f;
+    r.ent = h ? ent[i] : 0.f;
+    r.active = any && (r.g != 0.f || r.h != 0.f);
+    r.gs = 1.f;
+    if constexpr (DT == DT_F16) {
+      const float m = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
+      int e = 0;
+      if (r.active && m <= __FLT_MAX__) {
+        (void)frexpf(m, &e);
+        e = min(max(e, -120), 120);
+        r.gs = ldexpf(1.f, e);
+        r.g *= ldexpf(1.f, -e);
+        r.h *= ldexpf(1.f, -e);
+      }
+    }
+    r.pad = 0;
+    out[i] = r;
+  }
+}
+
+// The largest gs of an instance's active rows.
+__global__ __launch_bounds__(1024) void grad_gsmax_kernel(const RowGrad* __restrict__ rows,
+                                                          int64_t M, float* __restrict__ gsmax) {
+  __shared__ float s[16];
+  const int64_t b = blockIdx.x;
+  float m = 0.f;
+  for (int64_t i = threadIdx.x; i < M; i += 1024)
+    if (rows[b * M + i].active) m = __builtin_fmaxf(m, rows[b * M + i].gs);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
+  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < 16; ++i) m = __builtin_fmaxf(m, s[i]);
+    gsmax[b] = m > 0.f ? m : 1.f;
+  }
+}
+
+// in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance -> out [nb, C, ldo], zeros up to
+// ldo.  Rows that take no part become zeros: of X those without a gradient (the others
+// times gs / gsmax for fp16), of W the forbidden tokens.
+template <int DT>
+__global__ __launch_bounds__(256) void transpose_kernel(
+    const uint16_t* __restrict__ in, int64_t R, int C, int64_t r0, int64_t nr, int64_t ldo,
+    const RowGrad* __restrict__ rows, const float* __restrict__ gsmax,
+    const float* __restrict__ bias, uint16_t* __restrict__ out) {
+  __shared__ uint16_t tile[64][66];
+  const int64_t b = blockIdx.z, rt = (int64_t)blockIdx.x * 64;
+  const int ct = blockIdx.y * 64, t = threadIdx.x;
+  in += b * R * C;
+  for (int i = t; i < 64 * 64; i += 256) {
+    const int64_t r = rt + i / 64;
+    const int c = ct + i % 64;
+    uint16_t v = 0;
+    if (r < nr && c < C) {
+      bool use = true;
+      float f = 1.f;
+      if (rows) {
+        const RowGrad& g = rows[b * R + r0 + r];
+        use = g.active;
+        if (DT == DT_F16) f = g.gs / gsmax[b];
+      }
+      if (bias) use = bias[b * R + r0 + r] != NEG_INF;
+      if (use) {
+        v = in[(r0 + r) * C + c];
+        if (DT == DT_F16 && rows) v = Elem<DT>::narrow(Elem<DT>::widen(v) * f);
+      }
+    }
+    tile[i / 64][i % 64] = v;
+  }
+  __syncthreads();
+  out += b * C * ldo;
+  for (int i = t; i < 64 * 64; i += 256) {
+    const int c = ct + i / 64;
+    const int64_t r = rt + i % 64;
+    if (c < C && r < ldo) out[c * ldo + r] = tile[i % 64][i / 64];
+  }
+}
+
+struct DzArgs {
+  const char *X, *W;
+  const float* bias;
+  const RowGrad* rows;
+  int64_t xs, ws;   // instance strides in bytes
+  int64_t M, ld;
+  int V, v0, nv;    // all table rows; the block of them
+  int chunks;
+  float scale;
+  uint16_t *dz, *dzt;  // [nb, M, Vp], [nb, Vp, Mp]
+  int64_t Vp, Mp;
+};
+
+// dz of 256 positions by 256 table rows, rounded to 16 bits, and its transpose: the
+// tile goes through LDS so that both are written in whole lines.
+template <int DT, bool BIAS>
+__global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
+  using Z = NtSize<2, BIAS>;
+  __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
+  static_assert(Z::SMEM >= 256 * 512, "the tile fits the stages");
+  const int64_t b = blockIdx.z;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  NtIn in;
+  in.A = a.W + b * a.ws;
+  in.B = a.X + b * a.xs;
+  in.bias = BIAS ? a.bias + b * a.V : nullptr;
+  in.lda = in.ldb = a.ld;
+  in.nA = a.v0 + a.nv;
+  in.nB = (int)a.M;
+  in.a0 = a.v0 + blockIdx.y * 256;
+  in.b0 = blockIdx.x * LP_BB;
+  in.c0 = 0;
+  in.c1 = a.chunks;
+  in.nblk = 1;
+  NtLoop<DT, 2, BIAS> loop;
+  loop.init(in, smem);
+  const int wp = loop.wp, wc = loop.wc;
+  // row rl of the tile: 16-byte chunk c at c ^ f(rl), so that lanes 1 or 8 rows apart
+  // meet different banks
+  auto at = [](int rl, int c) {
+    return rl * 512 + ((c ^ (((((rl & 7) ^ ((rl >> 5) & 7))) << 2) | ((rl >> 3) & 3))) << 4);
+  };
+  auto epi = [&](f32x16(&acc)[4][2], int, const float* bias) {
+    float bz[2][16];
+    if constexpr (BIAS) {
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) bz[tc][4 * q + r] = x[r];
+        }
+    }
+    __syncthreads();  // every wave has read its last stage (and its bias)
+#pragma unroll
+    for (int tp = 0; tp < 4; ++tp) {
+      const int rl = wp * 128 + tp * 32 + n;
+      RowGrad rg;
+      rg.active = 0;
+      if (in.b0 + rl < a.M) rg = a.rows[b * a.M + in.b0 + rl];
+      const int v0 = in.a0 + wc * 64 + 4 * h;
+#pragma unroll
+      for (int tc = 0; tc < 2; ++tc)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          uint16_t w[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int j = 4 * q + r, v = v0 + tc * 32 + 8 * q + r;
+            float z = acc[tp][tc][j] * a.scale;
+            bool use = rg.active && v < in.nA;
+            if constexpr (BIAS) {
+              z = __builtin_fmaf(acc[tp][tc][j], a.scale, bz[tc][j]);
+              use = use && bz[tc][j] != NEG_INF;
+            }
+            const float lp = z - rg.lse;
+            const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
+            float dz = -p * __builtin_fmaf(rg.h, __builtin_fmaxf(lp, -1e30f) + rg.ent, rg.g);
+            if (v == rg.target) dz += rg.g;
+            if (DT == DT_F16) dz *= F16_UP;
+            w[r] = use ? Elem<DT>::narrow(dz) : (uint16_t)0;
+          }
+          const int c = wc * 8 + tc * 4 + q;
+          nt_at<uint2>(smem, at(rl, c) + 8 * h) =
+              make_uint2(w[0] | ((uint32_t)w[1] << 16), w[2] | ((uint32_t)w[3] << 16));
+        }
+    }
+    __syncthreads();
+  };
+  loop.run(epi);
+
+  const int64_t vb = in.a0 - a.v0;  // within the block of table rows
+  uint16_t* dz = a.dz + b * a.M * a.Vp;
+  uint16_t* dzt = a.dzt + b * a.Vp * a.Mp;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < 256 * 32; i += NT_T) {
+    const int rl = i >> 5, c = i & 31;
+    if (in.b0 + rl < a.M && vb + 8 * c < a.Vp)
+      *reinterpret_cast<uint4*>(dz + (in.b0 + rl) * a.Vp + vb + 8 * c) = nt_at<uint4>(smem, at(rl, c));
+  }
+#pragma unroll 2
+  for (int i = threadIdx.x; i < 128 * 32; i += NT_T) {
+    const int mo = i & 31, vp = i >> 5;  // 8 positions, 2 table rows
+    if (vb + 2 * vp >= a.Vp || in.b0 + 8 * mo >= a.Mp) continue;
+    uint32_t x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = nt_at<uint32_t>(smem, at(8 * mo + e, vp >> 2) + (vp & 3) * 4);
+    uint32_t lo[4], hi[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      lo[e] = (x[2 * e] & 0xffffu) | (x[2 * e + 1] << 16);
+      hi[e] = (x[2 * e] >> 16) | (x[2 * e + 1] & 0xffff0000u);
+    }
+    uint16_t* o = dzt + (vb + 2 * vp) * a.Mp + in.b0 + 8 * mo;
+    *reinterpret_cast<uint4*>(o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    *reinterpret_cast<uint4*>(o + a.Mp) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  }
+}
+
+// ---- the two products of the gradient ----------------------------------------------
+// out[r, d] = sum over c of At[d, c] Br[r, c]: At a transposed copy (D rows), Br dz or
+// its transpose.  Shares of the contraction go to `part` in fp32; whole ones are
+// written in 16 bits, or added to `acc` (dX over several blocks of table rows).
+enum OutMode { OUT_16 = 0, OUT_PART = 1, OUT_FIRST = 2, OUT_ADD = 3 };
+struct OutArgs {
+  const char *At, *Br;
+  int64_t as, bs;      // instance strides in bytes
+  int64_t ld;          // bytes of a row of either
+  int64_t R, os;       // rows, rows between instances of the output
+  int D, chunks, per;  // chunks of the contraction, stages of a share
+  int splits, mode;
+  float factor;
+  const RowGrad* rows;  // times rows[r].gs, if given
+  const float* gsmax;   // times gsmax[b], if given
+  uint16_t* out;
+  float* f32;          // part [nb, splits, R, D] or acc [R, D]
+};
+
+__device__ __forceinline__ float out_factor(float f, const RowGrad* rows, const float* gsmax,
+                                            int64_t b, int64_t os, int64_t r) {
+  if (rows) f *= rows[b * os + r].gs;
+  if (gsmax) f *= gsmax[b];
+  return f;
+}
+
+template <int DT, int TCW>
+__global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
+  using Z = NtSize<TCW, false>;
+  __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
+  const int ndb = (a.D + Z::BA - 1) / Z::BA;
+  const int64_t b = blockIdx.z;
+  const int sp = blockIdx.y;
+  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  NtIn in;
+  in.A = a.At + b * a.as;
+  in.B = a.Br + b * a.bs;
+  in.bias = nullptr;
+  in.lda = in.ldb = a.ld;
+  in.nA = a.D;
+  in.nB = (int)a.R;
+  in.a0 = (blockIdx.x % ndb) * Z::BA;
+  in.b0 = (blockIdx.x / ndb) * LP_BB;
+  in.c0 = sp * a.per * 4;
+  in.c1 = min(a.chunks, in.c0 + a.per * 4);
+  in.nblk = 1;
+  NtLoop<DT, TCW, false> loop;
+  loop.init(in, smem);
+  const int wp = loop.wp, wc = loop.wc;
+  auto epi = [&](f32x16(&acc)[4][TCW], int, const float*) {
+#pragma unroll
+    for (int tp = 0; tp < 4; ++tp) {
+      const int64_t r = in.b0 + wp * 128 + tp * 32 + n;
+      if (r >= a.R) continue;
+      const float f = a.mode == OUT_16 ? out_factor(a.factor, a.rows, a.gsmax, b, a.os, r) : 1.f;
+      uint16_t* o = a.out + (b * a.os + r) * a.D;
+      float* p = a.mode == OUT_PART ? a.f32 + ((b * a.splits + sp) * a.R + r) * a.D : a.f32 + r * a.D;
+#pragma unroll
+      for (int tc = 0; tc < TCW; ++tc)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int d = in.a0 + (wc * TCW + tc) * 32 + 8 * q + 4 * h;
+          if (a.mode == OUT_16) {
+            uint16_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = Elem<DT>::narrow(acc[tp][tc][4 * q + e] * f);
+            if (a.D % 4 == 0) {
+              if (d < a.D)
+                *reinterpret_cast<uint2*>(o + d) =
+                    make_uint2(w[0] | ((uint32_t)w[1] << 16), w[2] | ((uint32_t)w[3] << 16));
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (d + e < a.D) o[d + e] = w[e];
+            }
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d + e < a.D) {
+                float v = acc[tp][tc][4 * q + e];
+                if (a.mode == OUT_ADD) v += p[d + e];
+                p[d + e] = v;
+              }
+          }
+        }
+    }
+  };
+  loop.run(epi);
+}
+
+// out[b, r, d] = factor * sum over the shares of part[b, s, r, d].
+template <int DT>
+__global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs a, int64_t nb) {
+  const int64_t n = a.R * a.D;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < nb * n; i += (int64_t)gridDim.x * 256) {
+    const int64_t b = i / n, j = i % n, r = j / a.D;
+    const float* p = a.f32 + b * a.splits * n + j;
+    float v = 0.f;
+    for (int s = 0; s < a.splits; ++s) v += p[s * n];
+    a.out[b * a.os * a.D + j] =
+        Elem<DT>::narrow(v * out_factor(a.factor, a.rows, a.gsmax, b, a.os, r));
+  }
+}
+
+// ---- launchers -------------------------------------------------------------------
+template <int DT>
+hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s) {
+  hipError_t e;
+  const char *X = (const char*)a.X, *W = (const char*)a.W;
+  if (w.Dk != a.D) {
+    if ((e = launch_pad_rows(X, a.B * a.M, a.D, w.Dk, 2, w.xpad, s)) != hipSuccess) return e;
+    if ((e = launch_pad_rows(W, a.B * a.V, a.D, w.Dk, 2, w.wpad, s)) != hipSuccess) return e;
+    X = (const char*)w.xpad;
+    W = (const char*)w.wpad;
+  }
+  for (int64_t m0 = 0; m0 < a.M; m0 += w.plan.rows) {
+    const int64_t rows = std::min(w.plan.rows, a.M - m0);
+    ScoreArgs q;
+    q.X = X + m0 * w.Dk * 2;
+    q.W = W;
+    q.bias = a.bias;
+    q.target = a.target ? a.target + m0 : nullptr;
+    q.xs = a.M * w.Dk * 2;
+    q.ws = a.V * w.Dk * 2;
+    q.ts = a.M;
+    q.rows = rows;
+    q.ld = w.Dk * 2;
+    q.V = (int)a.V;
+    q.chunks = (int)(w.Dk / 8);
+    q.scale = a.scale;
+    q.grid = ScoreGrid{(int)((rows + LP_BB - 1) / LP_BB), w.plan.splits};
+    q.part = w.part;
+    q.zt = w.zt;
+    q.z = w.z;
+    q.gmax = w.gmax;
+    q.ldz = w.ldz;
+    q.groups = w.groups;
+    const dim3 grid(score_blocks(q.grid), (unsigned)a.B);
+    if (a.bias) {
+      if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
+      else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
+    } else {
+      if (a.k) score_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(q);
+      else score_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(q);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    FinishArgs f;
+    f.part = w.part;
+    f.zt = w.zt;
+    f.z = w.z;
+    f.gmax = w.gmax;
+    f.target = q.target;
+    f.rows = rows;
+    f.ts = a.M;
+    f.ldz = w.ldz;
+    f.groups = w.groups;
+    f.splits = w.plan.splits;
+    f.V = (int)a.V;
+    f.k = a.k;
+    f.logprob = a.logprob + m0;
+    f.entropy = a.entropy ? a.entropy + m0 : nullptr;
+    f.lse = a.lse + m0;
+    f.top_idx = a.top_idx + m0 * a.k;
+    f.top_logprob = a.top_logprob + m0 * a.k;
+    const dim3 fgrid((unsigned)rows, (unsigned)a.B);
+    if (a.k) logprobs_finish_kernel<true><<<fgrid, 64, w.groups * 4, s>>>(f);
+    else logprobs_finish_kernel<false><<<fgrid, 64, 0, s>>>(f);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <int DT>
+hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
+  const bool narrow = q.D <= 128;
+  const int ba = narrow ? 128 : 256, nst = (q.chunks + 3) / 4;
+  q.per = (nst + splits - 1) / splits;
+  q.splits = (nst + q.per - 1) / q.per;
+  const dim3 grid((unsigned)((q.D + ba - 1) / ba * ((q.R + LP_BB - 1) / LP_BB)), (unsigned)q.splits,
+                  (unsigned)nb);
+  if (narrow) out_kernel<DT, 1><<<grid, NT_T, 0, s>>>(q);
+  else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(q);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || q.mode != OUT_PART) return e;
+  const int64_t n = nb * q.R * q.D;
+  out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, nb);
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
+  hipError_t e;
+  const char *X = (const char*)a.X, *W = (const char*)a.W;
+  if (w.Dk != a.D) {
+    if ((e = launch_pad_rows(X, a.B * a.M, a.D, w.Dk, 2, w.xpad, s)) != hipSuccess) return e;
+    if ((e = launch_pad_rows(W, a.B * a.V, a.D, w.Dk, 2, w.wpad, s)) != hipSuccess) return e;
+    X = (const char*)w.xpad;
+    W = (const char*)w.wpad;
+  }
+  const int64_t rows = a.B * a.M;
+  grad_rows_kernel<DT><<<dim3((unsigned)std::min<int64_t>((rows + 255) / 256, 1 << 16)), 256, 0, s>>>(
+      a.target, a.lse, a.entropy, a.g, a.h, a.bias, rows, a.M, (int)a.V, w.rows);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  constexpr bool f16 = DT == DT_F16;
+  if (f16) {
+    grad_gsmax_kernel<<<dim3((unsigned)a.B), 1024, 0, s>>>(w.rows, a.M, w.gsmax);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
+    const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);
+    const RowGrad* rg = w.rows + b0 * a.M;
+    const float* gsmax = f16 ? w.gsmax + b0 : nullptr;
+    const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
+    transpose_kernel<DT><<<dim3((unsigned)(w.Mp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
+        (const uint16_t*)a.X + b0 * a.M * a.D, a.M, (int)a.D, 0, a.M, w.Mp, rg, gsmax, nullptr,
+        (uint16_t*)w.xt);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
+      const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64;
+      transpose_kernel<DT><<<dim3((unsigned)(vp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
+          (const uint16_t*)a.W + b0 * a.V * a.D, a.V, (int)a.D, v0, nv, vp, nullptr, nullptr, bias,
+          (uint16_t*)w.wt);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      DzArgs d;
+      d.X = X + b0 * a.M * w.Dk * 2;
+      d.W = W + b0 * a.V * w.Dk * 2;
+      d.bias = bias;
+      d.rows = rg;
+      d.xs = a.M * w.Dk * 2;
+      d.ws = a.V * w.Dk * 2;
+      d.M = a.M;
+      d.ld = w.Dk * 2;
+      d.V = (int)a.V;
+      d.v0 = (int)v0;
+      d.nv = (int)nv;
+      d.chunks = (int)(w.Dk / 8);
+      d.scale = a.scale;
+      d.dz = (uint16_t*)w.dz;
+      d.dzt = (uint16_t*)w.dzt;
+      d.Vp = vp;
+      d.Mp = w.Mp;
+      const dim3 grid((unsigned)((a.M + LP_BB - 1) / LP_BB), (unsigned)((nv + 255) / 256), (unsigned)nb);
+      if (a.bias) dz_kernel<DT, true><<<grid, NT_T, 0, s>>>(d);
+      else dz_kernel<DT, false><<<grid, NT_T, 0, s>>>(d);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+
+      const bool whole = w.Vc >= a.V;  // one block of table rows
+      OutArgs q{};
+      q.D = (int)a.D;
+      // dX: positions by D, over the table rows of this block
+      q.At = (const char*)w.wt;
+      q.Br = (const char*)w.dz;
+      q.ld = vp * 2;
+      q.as = a.D * q.ld;
+      q.bs = a.M * q.ld;
+      q.R = q.os = a.M;
+      q.chunks = (int)(vp / 8);
+      q.factor = f16 ? a.scale / F16_UP : a.scale;
+      q.rows = f16 ? rg : nullptr;
+      q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
+      q.mode = !whole ? (v0 ? OUT_ADD : OUT_FIRST) : w.sx > 1 ? OUT_PART : OUT_16;
+      q.f32 = whole ? w.part : w.accx;
+      if ((e = launch_out<DT>(q, nb, whole ? w.sx : 1, s)) != hipSuccess) return e;
+      // dW: the block's table rows by D, over the positions
+      q.At = (const char*)w.xt;
+      q.Br = (const char*)w.dzt;
+      q.ld = w.Mp * 2;
+      q.as = a.D * q.ld;
+      q.bs = vp * q.ld;
+      q.R = nv;
+      q.os = a.V;
+      q.chunks = (int)(w.Mp / 8);
+      q.rows = nullptr;
+      q.gsmax = gsmax;
+      q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
+      q.mode = w.sw > 1 ? OUT_PART : OUT_16;
+      q.f32 = w.part;
+      if ((e = launch_out<DT>(q, nb, w.sw, s)) != hipSuccess) return e;
+    }
+    if (w.Vc < a.V) {  // dX from its fp32 sums
+      OutArgs q{};
+      q.D = (int)a.D;
+      q.R = q.os = a.M;
+      q.splits = 1;
+      q.factor = f16 ? a.scale / F16_UP : a.scale;
+      q.rows = f16 ? rg : nullptr;
+      q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
+      q.f32 = w.accx;
+      const int64_t n = a.M * a.D;
+      out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, 1);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+}  // namespace fkm

@@ -1,0 +1,214 @@
+// tokens_api.hip -- the C ABI of the operators on token tables (declared in
+// include/flashtokens.h): argument validation on the host before anything touches
+// the GPU, workspace carving and the choice of shares.
+#include <algorithm>
+#include <cmath>
+
+#include "../../include/flashtokens.h"
+#include "tokens_internal.h"
+
+namespace fkm {
+
+namespace {
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+int check_tokens(int64_t B, int64_t M, int64_t V, int64_t D, int dt) {
+  if (B < 1 || M < 1 || V < 1 || D < 1) return FKM_ERR_INVALID_ARG;
+  if (dt != DT_F32 && dt != DT_BF16 && dt != DT_F16) return FKM_ERR_INVALID_ARG;
+  if (B > 65535 || M > TOK_MAX_M || V > TOK_MAX_V || D > TOK_MAX_D) return FKM_ERR_UNSUPPORTED;
+  return FKM_OK;
+}
+int check_scores(int64_t B, int64_t M, int64_t V, int64_t D, int64_t k, int dt) {
+  const int rc = check_tokens(B, M, V, D, dt);
+  if (rc) return rc;
+  if (k < 0 || k > V) return FKM_ERR_INVALID_ARG;
+  if (dt == DT_F32 || k > TOK_MAX_K) return FKM_ERR_UNSUPPORTED;
+  return FKM_OK;
+}
+int check_optional(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!aligned16(p)) return FKM_ERR_INVALID_ARG;
+  return FKM_OK;
+}
+
+struct Taker {
+  char* p;
+  size_t o = 0;
+  template <typename T>
+  void operator()(T*& out, size_t bytes) {
+    out = (T*)(p ? p + o : nullptr);
+    o = (o + bytes + 255) & ~size_t(255);
+  }
+};
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// At most this many workgroups come of sharing out column blocks or a contraction:
+// two rounds on 256 CUs (contractions) or four (columns).
+constexpr int64_t SCORE_WGS = 1024, OUT_WGS = 512;
+
+// Shares of the column blocks: the number with the least rounds of 256 workgroups
+// times what one takes, its blocks and about six stages of filling and emptying.
+// Multiples of 8 from 8 on, so that each XCD gets as many.
+int score_splits(int64_t wgs, int64_t nvb, int64_t stages) {
+  const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / wgs));
+  int best = 1;
+  double least = HUGE_VAL;
+  for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
+    const double us = (double)cdiv(wgs * s, 256) * ((double)(cdiv(nvb, s) * stages) + 6);
+    if (us < least) least = us, best = (int)s;
+  }
+  return best;
+}
+
+LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D, int k) {
+  LogprobsWs w{};
+  Taker take{(char*)base};
+  w.Dk = up(D, 8);
+  w.ldz = up(V, 256);
+  w.groups = w.ldz / LP_GROUP;
+  w.plan.rows = M;
+  if (k) w.plan.rows = std::min(M, std::max<int64_t>(LP_SCORE_BYTES / (B * w.ldz * 4) / 256, 1) * 256);
+  const int64_t nmb = cdiv(w.plan.rows, LP_BB), wgs = nmb * B;
+  w.plan.splits = score_splits(wgs, w.ldz / 256, cdiv(w.Dk, LP_DC));
+  take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
+  take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
+  // B x splits x rows, for any number of shares that these or fewer rows would get
+  take(w.part, (size_t)(std::max(SCORE_WGS, wgs) * LP_BB) * sizeof(float4));
+  take(w.zt, (size_t)(B * w.plan.rows) * 4);
+  take(w.gmax, k ? (size_t)(B * w.plan.rows * w.groups) * 4 : 0);
+  take(w.z, k ? (size_t)(B * w.plan.rows * w.ldz) * 4 : 0);
+  w.total = take.o;
+  return w;
+}
+
+// Shares of a contraction of `stages` stages over `tiles` output tiles: enough to
+// fill the chip, of at least 16 stages.
+int out_splits(int64_t tiles, int64_t stages) {
+  return (int)std::max<int64_t>(1, std::min(OUT_WGS / tiles, stages / 16));
+}
+
+GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
+  GradWs w{};
+  Taker take{(char*)base};
+  w.Dk = up(D, 8);
+  w.Mp = up(M, 64);
+  const int64_t Vall = up(V, 64), one = w.Mp * Vall * 4;
+  w.nb = B * one <= LP_DZ_BYTES ? (int)B : 1;
+  w.Vc = w.nb * one <= LP_DZ_BYTES || V <= 256
+             ? V : std::min(V, std::max<int64_t>(LP_DZ_BYTES / (4 * w.Mp) / 256, 1) * 256);
+  w.Vp = up(w.Vc, 64);
+  const int64_t ba = D <= 128 ? 128 : 256, dt = cdiv(D, ba);
+  w.sx = out_splits(w.nb * cdiv(M, LP_BB) * dt, w.Vp / LP_DC);
+  w.sw = out_splits(w.nb * cdiv(w.Vc, LP_BB) * dt, w.Mp / LP_DC);
+  take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
+  take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
+  take(w.rows, (size_t)(B * M) * sizeof(RowGrad));
+  take(w.gsmax, (size_t)B * 4);
+  // sizes that never shrink as M grows, whatever the plan then is
+  const size_t dz = (size_t)std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2);
+  take(w.dz, dz);
+  take(w.dzt, dz);
+  take(w.xt, (size_t)(B * D * w.Mp) * 2);
+  take(w.wt, (size_t)(B * D * Vall) * 2);
+  take(w.accx, w.Vc < V ? (size_t)(M * D) * 4 : 0);
+  const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
+  const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);
+  const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * D * (w.Mp / 512), cap);
+  take(w.part, (size_t)std::max(px, pw) * 4);
+  w.total = take.o;
+  return w;
+}
+
+}  // namespace
+
+}  // namespace fkm
+
+using namespace fkm;
+
+extern "C" {
+
+int tokens_embed(const void* W, int dtype, const int32_t* idx, int64_t B, int64_t M, int64_t V,
+                 int64_t D, float scale, void* out, void* stream) {
+  int rc;
+  if ((rc = check_ptrs({W, idx, out}))) return rc;
+  if ((rc = check_tokens(B, M, V, D, dtype))) return rc;
+  if ((rc = check_device())) return rc;
+  return hip_status(launch_embed(W, dtype, idx, B, M, V, D, scale, out, (hipStream_t)stream));
+}
+
+size_t tokens_embed_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int gdtype) {
+  if (check_tokens(B, M, V, D, gdtype) != FKM_OK) return 0;
+  return embed_grad_carve(nullptr, B, M, V, D).total;
+}
+
+int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, int64_t M,
+                      int64_t V, int64_t D, float scale, int accumulate, void* dW, int wdtype,
+                      void* ws, size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_ptrs({G, idx, dW}))) return rc;
+  if ((rc = check_tokens(B, M, V, D, gdtype))) return rc;
+  if (wdtype != gdtype && wdtype != DT_F32) return FKM_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < embed_grad_carve(nullptr, B, M, V, D).total)
+    return FKM_ERR_WORKSPACE;
+  if ((rc = check_device())) return rc;
+  return hip_status(launch_embed_grad(G, gdtype, idx, B, M, V, D, scale, accumulate != 0, dW, wdtype,
+                                      embed_grad_carve(ws, B, M, V, D), (hipStream_t)stream));
+}
+
+size_t tokens_logprobs_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int k,
+                                       int xdtype) {
+  if (check_scores(B, M, V, D, k, xdtype) != FKM_OK) return 0;
+  return logprobs_carve(nullptr, B, M, V, D, k).total;
+}
+
+int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
+                    const int32_t* target, int64_t B, int64_t M, int64_t V, int64_t D, float scale,
+                    int k, float* logprob, float* entropy, float* lse, int32_t* top_idx,
+                    float* top_logprob, void* ws, size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_ptrs({X, W, lse}))) return rc;
+  if ((rc = check_optional({bias, target, logprob, entropy, top_idx, top_logprob}))) return rc;
+  if (target && !logprob) return FKM_ERR_INVALID_ARG;
+  if (k > 0 && (!top_idx || !top_logprob)) return FKM_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
+  if ((rc = check_scores(B, M, V, D, k, xdtype))) return rc;
+  if (!ws || !aligned16(ws) || ws_bytes < logprobs_carve(nullptr, B, M, V, D, k).total)
+    return FKM_ERR_WORKSPACE;
+  if ((rc = check_device())) return rc;
+  const LogprobsArgs a{X, W, bias, target, B, M, V, D, scale, k, logprob, entropy, lse, top_idx,
+                       top_logprob};
+  const LogprobsWs w = logprobs_carve(ws, B, M, V, D, k);
+  return hip_status((xdtype == DT_BF16 ? launch_logprobs_bf16 : launch_logprobs_f16)(
+      a, w, (hipStream_t)stream));
+}
+
+size_t tokens_logprobs_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D,
+                                            int xdtype) {
+  if (check_scores(B, M, V, D, 0, xdtype) != FKM_OK) return 0;
+  return grad_carve(nullptr, B, M, V, D).total;
+}
+
+int tokens_logprobs_grad(const void* X, const void* W, int xdtype, const float* bias,
+                         const int32_t* target, const float* lse, const float* entropy,
+                         const float* grad_logprob, const float* grad_entropy, int64_t B, int64_t M,
+                         int64_t V, int64_t D, float scale, void* dX, void* dW, void* ws,
+                         size_t ws_bytes, void* stream) {
+  int rc;
+  if ((rc = check_ptrs({X, W, target, lse, grad_logprob, dX, dW}))) return rc;
+  if ((rc = check_optional({bias, entropy, grad_entropy}))) return rc;
+  if (grad_entropy && !entropy) return FKM_ERR_INVALID_ARG;
+  if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
+  if ((rc = check_scores(B, M, V, D, 0, xdtype))) return rc;
+  if (!ws || !aligned16(ws) || ws_bytes < grad_carve(nullptr, B, M, V, D).total)
+    return FKM_ERR_WORKSPACE;
+  if ((rc = check_device())) return rc;
+  const GradArgs a{X, W, bias, target, lse, entropy, grad_logprob, grad_entropy, B, M, V, D, scale,
+                   dX, dW};
+  const GradWs w = grad_carve(ws, B, M, V, D);
+  return hip_status((xdtype == DT_BF16 ? launch_logprobs_grad_bf16 : launch_logprobs_grad_f16)(
+      a, w, (hipStream_t)stream));
+}
+
+}  // extern "C"

@@ -1,0 +1,122 @@
+// tokens_internal.h -- limits, workspaces and launchers shared by the HIP
+// translation units of the operators on token tables (include/flashtokens.h).
+#pragma once
+
+#include <initializer_list>
+
+#include "fkm_internal.h"
+
+namespace fkm {
+
+constexpr int64_t TOK_MAX_M = 1 << 24, TOK_MAX_V = 1 << 20, TOK_MAX_D = 8192;
+constexpr int TOK_MAX_K = 32;
+
+// api.hip
+int check_device();
+int check_ptrs(std::initializer_list<const void*> ps);
+int hip_status(hipError_t e);
+
+// Positions sorted by token: a stable radix sort of (token, position), in as many
+// passes of at most 8 bits as the tokens take (update.hip).  keys / vals: [B, M]
+// each, the sorted ones in keys[0] / vals[0]; total[b] the number of positions
+// with a token.
+struct TokenSort {
+  int32_t *keys[2], *vals[2];
+  int32_t *hist, *bins;  // [B, 256, chunks], [B, 256]
+  int32_t* total;        // [B]
+};
+hipError_t launch_token_sort(const int32_t* idx, int64_t B, int64_t M, int64_t V,
+                             const TokenSort& t, hipStream_t s);
+
+hipError_t launch_embed(const void* W, int dt, const int32_t* idx, int64_t B, int64_t M, int64_t V,
+                        int64_t D, float scale, void* out, hipStream_t s);
+
+struct EmbedGradWs {
+  TokenSort sort;
+  float* carry;  // [B, slices, 2, D] sums of runs cut by slice ends
+  size_t total;
+};
+EmbedGradWs embed_grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D);
+hipError_t launch_embed_grad(const void* G, int gdt, const int32_t* idx, int64_t B, int64_t M,
+                             int64_t V, int64_t D, float scale, bool accumulate, void* dW, int wdt,
+                             const EmbedGradWs& w, hipStream_t s);
+
+// ---- scores against a table (logprobs.h) ----------------------------------------
+// Products are tiled 256 positions x 256 (or 128) table rows; contractions are cut
+// in stages of 32 elements.
+constexpr int LP_BB = 256, LP_DC = 32;
+// A scored row's columns come in groups of 64, whose best scores lead to the k best.
+constexpr int LP_GROUP = 64;
+
+// tokens_logprobs.  Rows are taken in blocks whose stored scores (k > 0 only) stay
+// within LP_SCORE_BYTES; column blocks of 256 are shared out over `splits`
+// workgroups a row block, whose softmax statistics are merged.
+constexpr int64_t LP_SCORE_BYTES = (int64_t)1 << 30;
+struct LogprobsPlan {
+  int64_t rows;    // rows of a block (all of M for k = 0)
+  int splits;      // shares of the column blocks, a workgroup each
+};
+struct LogprobsWs {
+  void *xpad, *wpad;  // rows of Dk elements, where D is no multiple of 8
+  float4* part;       // [B, splits, rows] max, sum, weighted sum of each share
+  float* zt;          // [B, rows] score of the target
+  float* gmax;        // [B, rows, groups] best score of each group (k > 0)
+  float* z;           // [B, rows, ldz] scores (k > 0)
+  int64_t Dk, ldz, groups;
+  LogprobsPlan plan;
+  size_t total;
+};
+
+struct LogprobsArgs {
+  const void *X, *W;
+  const float* bias;
+  const int32_t* target;
+  int64_t B, M, V, D;
+  float scale;
+  int k;
+  float *logprob, *entropy, *lse;
+  int32_t* top_idx;
+  float* top_logprob;
+};
+
+// tokens_logprobs_grad.  dz of a block of table rows (Vc of them; all, where it
+// fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in 16
+// bits, and both products read it and transposed copies of X and W.
+constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
+struct RowGrad {  // one position
+  float g, h;     // gradients of the log probability and the entropy, over `gs`
+  float lse, ent;
+  int target;     // -1: none
+  int active;     // takes part at all
+  float gs;       // a power of two: what dz of this row is divided by (fp16; else 1)
+  int pad;
+};
+struct GradWs {
+  void *xpad, *wpad;
+  RowGrad* rows;    // [B, M]
+  float* gsmax;     // [B] largest gs
+  void *dz, *dzt;   // [nb, M, Vp], [nb, Vp, Mp]
+  void *xt, *wt;    // [nb, D, Mp], [nb, D, Vp]
+  float* accx;      // [M, D] dX over the blocks of table rows, where there are several
+  float* part;      // [nb, splits, rows, D] shares of a contraction
+  int64_t Dk, Mp, Vp, Vc;
+  int nb;           // instances at a time (B or 1)
+  int sx, sw;       // shares of dX's and dW's contractions
+  size_t total;
+};
+
+struct GradArgs {
+  const void *X, *W;
+  const float* bias;
+  const int32_t* target;
+  const float *lse, *entropy, *g, *h;
+  int64_t B, M, V, D;
+  float scale;
+  void *dX, *dW;
+};
+hipError_t launch_logprobs_bf16(const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s);
+hipError_t launch_logprobs_f16(const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s);
+hipError_t launch_logprobs_grad_bf16(const GradArgs& a, const GradWs& w, hipStream_t s);
+hipError_t launch_logprobs_grad_f16(const GradArgs& a, const GradWs& w, hipStream_t s);
+
+}  // namespace fkm

@@ -17,6 +17,7 @@
 #include <type_traits>
 
 #include "fkm_device.h"
+#include "tokens_internal.h"
 
 namespace fkm {
 
@@ -1146,6 +1147,37 @@ hipError_t launch_update(const void* X, int dt, const int32_t* idx, const float*
       w.sums, w.carry, counts, w.off, C_prev, (int)K, (int)D, (int)w.n_red_chunks, (int)w.red_cr,
       C_out, nx);
   return hipGetLastError();
+}
+
+// Positions sorted by token for the gradient of a lookup: plain passes over (key,
+// value) arrays, alternating between the two pairs so that the last one writes
+// keys[0] / vals[0]; the first reads idx itself and drops ids outside [0, V).
+hipError_t launch_token_sort(const int32_t* idx, int64_t B, int64_t M, int64_t V,
+                             const TokenSort& t, hipStream_t s) {
+  const int bits = key_bits(V), passes = (bits + RADIX_MAX_BITS - 1) / RADIX_MAX_BITS;
+  const int nch = (int)((M + RADIX_CHUNK - 1) / RADIX_CHUNK);
+  const dim3 grid(nch, (unsigned)B);
+  int shift = 0;
+  for (int p = 0; p < passes; ++p) {
+    const int d = (bits - shift + passes - p - 1) / (passes - p), R = 1 << d;
+    const int out = (passes - 1 - p) & 1;
+    const int32_t* kin = p ? t.keys[1 - out] : idx;
+    const int32_t* vin = p ? t.vals[1 - out] : nullptr;
+    const int32_t* n = p ? t.total : nullptr;
+    hipError_t e;
+    radix_hist_kernel<<<grid, 256, 0, s>>>(kin, (int)M, (int)V, n, shift, R, nch, t.hist, 0, nullptr,
+                                           0);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    radix_scan_kernel<<<dim3(R, (unsigned)B), 256, 0, s>>>(t.hist, R, nch, RADIX_MAX_R, t.bins);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if ((e = launch_scatter<0>(d, grid, s, kin, vin, (int)M, (int)V, n, shift, nch,
+                               (const int32_t*)t.hist, (const int32_t*)t.bins,
+                               p ? (int32_t*)nullptr : t.total, t.keys[out], t.vals[out], 0, 0,
+                               (const int32_t*)nullptr, (int32_t*)nullptr)) != hipSuccess)
+      return e;
+    shift += d;
+  }
+  return hipSuccess;
 }
 
 }  // namespace fkm
