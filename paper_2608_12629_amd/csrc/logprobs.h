@@ -30,19 +30,27 @@ __device__ const uint4 nt_zero = {0, 0, 0, 0};
 
 // L2 -> LDS copies of 16 (or 4) bytes a lane into the wave's slots at `lds`, issued
 // by inline assembly so that only the explicit waits below govern them; M0 (the LDS
-// base) is set in the same statement, one wait state before the load reads it.
-__device__ __forceinline__ void nt_dma16(const void* src, char* lds) {
-  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+// base) is set in the same statement, one wait state before the load reads it.  From
+// a scalar base and 32-bit offsets, or from 64-bit addresses.
+__device__ __forceinline__ uint32_t nt_lds(char* lds) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
+}
+__device__ __forceinline__ void nt_dma16(const char* base, uint32_t off, char* lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
-               : "v"(src), "s"(base)
+               : "v"(off), "s"(base), "s"(nt_lds(lds))
                : "memory");
 }
-__device__ __forceinline__ void nt_dma4(const void* src, char* lds) {
-  const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off"
+__device__ __forceinline__ void nt_dma16(const void* src, char* lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
                :
-               : "v"(src), "s"(base)
+               : "v"(src), "s"(nt_lds(lds))
+               : "memory");
+}
+__device__ __forceinline__ void nt_dma4(const char* base, uint32_t off, char* lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
+               :
+               : "v"(off), "s"(base), "s"(nt_lds(lds))
                : "memory");
 }
 
@@ -90,20 +98,22 @@ struct NtFrag {
 template <int DT, int TCW, bool BIAS>
 struct NtLoop {
   using Z = NtSize<TCW, BIAS>;
-  const char *ap[TCW], *bp[2];
-  const float* biasp;
   NtIn in;
-  int tid, wave, cc, iblk, id, nds;  // the stage to load next: block iblk, stage id of it
+  // the stage to load next: block iblk, stage id of it; each operand's first row and
+  // chunk of that stage, and the thread's offsets from it (rows clamped)
+  const char *ab, *bb;
+  uint32_t ao[TCW], bo[2], biaso;
+  int tid, wave, cc, iblk, id, nds;
   int loff0, loff1, wp, wc;
   char* smem;
 
   __device__ __forceinline__ void block_rows(int blk) {
-    const int r = in.a0 + blk * Z::BA + (tid >> 2);
+    const int a0 = in.a0 + blk * Z::BA, last = in.nA - 1 - a0, r = tid >> 2;
+    ab = in.A + (int64_t)a0 * in.lda + in.c0 * 16;
 #pragma unroll
     for (int u = 0; u < TCW; ++u)
-      ap[u] = in.A + (int64_t)min(r + 128 * u, in.nA - 1) * in.lda + (in.c0 + cc) * 16;
-    if constexpr (BIAS)
-      biasp = in.bias + min(in.a0 + blk * Z::BA + (tid & (Z::BA - 1)), in.nA - 1);
+      ao[u] = (uint32_t)max(min(r + 128 * u, last), 0) * (uint32_t)in.lda + cc * 16;
+    if constexpr (BIAS) biaso = (uint32_t)min(tid & (Z::BA - 1), max(last, 0)) * 4;
   }
 
   __device__ __forceinline__ void init(const NtIn& i, char* sm) {
@@ -115,9 +125,10 @@ struct NtLoop {
     cc = (tid & 3) ^ nt_swz(tid >> 2);
     nds = (in.c1 - in.c0 + 3) / 4;
     iblk = id = 0;
+    bb = in.B + (int64_t)in.b0 * in.ldb + in.c0 * 16;
 #pragma unroll
     for (int u = 0; u < 2; ++u)
-      bp[u] = in.B + (int64_t)min(in.b0 + (tid >> 2) + 128 * u, in.nB - 1) * in.ldb + (in.c0 + cc) * 16;
+      bo[u] = (uint32_t)min((tid >> 2) + 128 * u, in.nB - 1 - in.b0) * (uint32_t)in.ldb + cc * 16;
     block_rows(0);
     // lane 32 h + n reads row (tile base + n), chunk 2 step + h
     loff0 = n * 64 + ((0 + h) ^ nt_swz(n)) * 16;
@@ -126,51 +137,100 @@ struct NtLoop {
     wc = wave >> 1;  // quarter of A's rows
   }
 
+  // Start the loads of the next stage.
   __device__ __forceinline__ void issue(char* buf) {
-    const bool in_range = in.c0 + id * 4 + cc < in.c1;
-    const int off = id * 64;
+    char* dst = buf + wave * 1024;
+    if (in.c0 + id * 4 + 4 <= in.c1) {
 #pragma unroll
-    for (int u = 0; u < TCW; ++u)
-      nt_dma16(in_range ? ap[u] + off : (const char*)&nt_zero, buf + (u * NT_T + wave * 64) * 16);
+      for (int u = 0; u < TCW; ++u) nt_dma16(ab, ao[u], dst + u * (NT_T * 16));
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      nt_dma16(in_range ? bp[u] + off : (const char*)&nt_zero,
-               buf + Z::AB + (u * NT_T + wave * 64) * 16);
-    if constexpr (BIAS) nt_dma4(biasp, buf + Z::AB + Z::BBY + wave * 256);
+      for (int u = 0; u < 2; ++u) nt_dma16(bb + id * 64, bo[u], dst + Z::AB + u * (NT_T * 16));
+    } else {  // the last stage of a contraction that is no whole number of them
+      const bool have = in.c0 + id * 4 + cc < in.c1;
+#pragma unroll
+      for (int u = 0; u < TCW; ++u)
+        nt_dma16(have ? ab + ao[u] : (const char*)&nt_zero, dst + u * (NT_T * 16));
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        nt_dma16(have ? bb + id * 64 + bo[u] : (const char*)&nt_zero, dst + Z::AB + u * (NT_T * 16));
+    }
+    if constexpr (BIAS)
+      nt_dma4((const char*)(in.bias + in.a0 + iblk * Z::BA), biaso, buf + Z::AB + Z::BBY + wave * 256);
+    ab += 64;
     if (++id == nds) {
       id = 0;
       block_rows(++iblk);
     }
   }
 
+  __device__ __forceinline__ void read_a(NtFrag<TCW>& f, char* buf, int lo, int tc) {
+    f.a[tc] = nt_at<uint4>(buf, (wc * TCW + tc) * 2048 + lo);
+  }
+  __device__ __forceinline__ void read_b(NtFrag<TCW>& f, char* buf, int lo, int tp) {
+    f.b[tp] = nt_at<uint4>(buf, Z::AB + (wp * 4 + tp) * 2048 + lo);
+  }
   __device__ __forceinline__ void read(NtFrag<TCW>& f, char* buf, int lo) {
 #pragma unroll
-    for (int tc = 0; tc < TCW; ++tc) f.a[tc] = nt_at<uint4>(buf, (wc * TCW + tc) * 2048 + lo);
+    for (int tc = 0; tc < TCW; ++tc) read_a(f, buf, lo, tc);
 #pragma unroll
-    for (int tp = 0; tp < 4; ++tp)
-      f.b[tp] = nt_at<uint4>(buf, Z::AB + (wp * 4 + tp) * 2048 + lo);
+    for (int tp = 0; tp < 4; ++tp) read_b(f, buf, lo, tp);
   }
 
-  __device__ __forceinline__ void mfma(f32x16 (&acc)[4][TCW], const NtFrag<TCW>& f) {
+  // The MFMAs of one 16-element step on `f`, in a fixed order with everything else that
+  // the wave has to issue between them: the next step's fragments into `g` from `buf`,
+  // then (LOAD, if there is a stage left to load) the loads of a later stage into
+  // `ahead`.  The matrix cores take 32 cycles an MFMA, so what stands between two of
+  // them is free; in a block of its own, after the barrier and before the MFMAs, it cost
+  // both waves of a SIMD the same idle cycles.
+  template <bool LOAD>
+  __device__ __forceinline__ void step(f32x16 (&acc)[4][TCW], const NtFrag<TCW>& f, NtFrag<TCW>& g,
+                                       char* buf, int lo, char* ahead, bool more) {
+    constexpr int N = 4 * TCW, R = TCW + 4;
 #pragma unroll
-    for (int tp = 0; tp < 4; ++tp)
+    for (int m = 0; m < N; ++m) {
+      const int tp = m / TCW, tc = m % TCW;
+      acc[tp][tc] = mfma32_chunk<DT>(f.a[tc], f.b[tp], acc[tp][tc]);
+      __builtin_amdgcn_sched_barrier(0);
+      // two reads after each of the first MFMAs (a step has at least 4)
 #pragma unroll
-      for (int tc = 0; tc < TCW; ++tc) acc[tp][tc] = mfma32_chunk<DT>(f.a[tc], f.b[tp], acc[tp][tc]);
+      for (int i = 2 * m; i < 2 * m + 2; ++i) {
+        if (i < TCW) read_a(g, buf, lo, i);
+        else if (i < R) read_b(g, buf, lo, i - TCW);
+      }
+      if constexpr (LOAD) {
+        if (m == N / 2 && more) issue(ahead);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
   }
+
+  // Stage s (its first step's fragments are in f0): read the second step's beside the
+  // first step's MFMAs, wait for stage s + 1, then beside the second step's MFMAs read
+  // stage s + 1's first fragments and start stage s + 3 into the buffer of stage s - 1,
+  // which every wave has finished.  Past the last stage the reads bring values that
+  // nobody uses; one path for all stages keeps the accumulators in their registers.
+  __device__ __forceinline__ void stage(int s, int S, f32x16 (&acc)[4][TCW], NtFrag<TCW>& f0,
+                                        NtFrag<TCW>& f1) {
+    step<false>(acc, f0, f1, at(s), loff1, nullptr, false);
+    // (vmcnt counts in issue order: an epilogue's stores only make the wait longer)
+    if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
+    else nt_wait_and_sync<0>();
+    step<true>(acc, f1, f0, at(s + 1), loff0, at(s + 3), s + 3 < S);
+  }
+  __device__ __forceinline__ char* at(int s) { return smem + (s & 3) * Z::STAGE; }
 
   // epi(acc, block, bias of the block in LDS) after each block
   template <class Epi>
   __device__ __forceinline__ void run(Epi&& epi) {
     const int S = in.nblk * nds;
-    auto buf = [&](int s) { return smem + (s & 3) * Z::STAGE; };
-    issue(buf(0));
-    if (1 < S) issue(buf(1));
-    if (2 < S) issue(buf(2));
+    issue(at(0));
+    if (1 < S) issue(at(1));
+    if (2 < S) issue(at(2));
     if (2 < S) nt_wait_and_sync<2 * Z::LOADS>();
     else if (1 < S) nt_wait_and_sync<Z::LOADS>();
     else nt_wait_and_sync<0>();
     NtFrag<TCW> f0, f1;
-    read(f0, buf(0), loff0);
+    read(f0, at(0), loff0);
     f32x16 acc[4][TCW];
     int s = 0;
     for (int g = 0; g < in.nblk; ++g) {
@@ -180,20 +240,8 @@ struct NtLoop {
         for (int tc = 0; tc < TCW; ++tc)
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc[tp][tc][j] = 0.f;
-      for (int d = 0; d < nds; ++d, ++s) {
-        // stage s: its second step's fragments, the first step's MFMAs, then wait for
-        // stage s + 1, start stage s + 3 into the buffer of stage s - 1 (which every
-        // wave has finished), read stage s + 1's first fragments
-        read(f1, buf(s), loff1);
-        mfma(acc, f0);
-        // (vmcnt counts in issue order: an epilogue's stores only make the wait longer)
-        if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
-        else nt_wait_and_sync<0>();
-        if (s + 3 < S) issue(buf(s + 3));
-        if (s + 1 < S) read(f0, buf(s + 1), loff0);
-        mfma(acc, f1);
-      }
-      epi(acc, g, reinterpret_cast<const float*>(buf(s - 1) + Z::AB + Z::BBY));
+      for (const int end = s + nds; s < end; ++s) stage(s, S, acc, f0, f1);
+      epi(acc, g, reinterpret_cast<const float*>(at(s - 1) + Z::AB + Z::BBY));
     }
   }
 };
@@ -221,30 +269,20 @@ __device__ __forceinline__ Stat stat_merge(Stat a, Stat b) {
 }
 
 // ---- scores --------------------------------------------------------------------
-// One workgroup: 256 rows of X by a share of the column blocks.  Share sp of the columns and
-// row block mb are chosen so that the workgroups of an XCD (ids go round-robin over
-// the eight) share a few column shares and row blocks through its L2.
-struct ScoreGrid {
-  int nmb, splits;  // row blocks, shares of the column blocks (all within one of a size)
-};
-__device__ __forceinline__ bool score_place(const ScoreGrid& g, int id, int& mb, int& sp) {
-  if (g.splits >= 8) {  // shares dealt to the XCDs; 8 row blocks at a time, shares inside
-    const int xcd = id & 7, j = id >> 3, sx = (g.splits + 7) / 8;
-    const int gm = min(8, g.nmb), sup = j / (gm * sx), r = j % (gm * sx);
-    mb = sup * gm + r % gm;
-    sp = xcd * sx + r / gm;
-    return mb < g.nmb && sp < g.splits;
-  }
-  sp = id % g.splits;
-  mb = id / g.splits;
-  return mb < g.nmb;
-}
-inline unsigned score_blocks(const ScoreGrid& g) {
-  if (g.splits < 8) return (unsigned)(g.nmb * g.splits);
-  const int sx = (g.splits + 7) / 8, gm = std::min(8, g.nmb);
-  return (unsigned)((g.nmb + gm - 1) / gm * gm * sx * 8);
+// Workgroup `id`: its blocks of A and B and instance; false past the last one.
+__device__ __forceinline__ bool raster_place(const Raster& r, int id, int& a, int& b, int64_t& inst) {
+  const int xcd = id & 7, j = id >> 3, size = r.ga * r.gb;
+  const int64_t sup = (int64_t)(j / size) * 8 + xcd;
+  const int nsa = (r.na + r.ga - 1) / r.ga, nsb = (r.nb + r.gb - 1) / r.gb, in = j % size;
+  inst = sup / (nsa * nsb);
+  const int at = (int)(sup % (nsa * nsb));
+  a = at / nsb * r.ga + in / r.gb;
+  b = at % nsb * r.gb + in % r.gb;
+  return sup < r.supers && a < r.na && b < r.nb;
 }
 
+// One workgroup: 256 rows of X by a share of the column blocks (all shares within one
+// block of a size).
 struct ScoreArgs {
   const char *X, *W;
   const float* bias;
@@ -254,7 +292,7 @@ struct ScoreArgs {
   int64_t ld;            // bytes of a row
   int V, chunks;         // 16-byte chunks of a row
   float scale;
-  ScoreGrid grid;
+  Raster grid;           // shares by row blocks
   float4* part;          // [B, splits, rows]
   float* zt;             // [B, rows]
   float *z, *gmax;       // [B, rows, ldz], [B, rows, groups]
@@ -266,11 +304,11 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   using Z = NtSize<2, BIAS>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   int mb, sp;
-  if (!score_place(a.grid, blockIdx.x, mb, sp)) return;
-  const int64_t b = blockIdx.y;
+  int64_t b;
+  if (!raster_place(a.grid, blockIdx.x, sp, mb, b)) return;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   const int64_t nvb = (a.V + 255) / 256;
-  const int blk0 = (int)(nvb * sp / a.grid.splits), blk1 = (int)(nvb * (sp + 1) / a.grid.splits);
+  const int blk0 = (int)(nvb * sp / a.grid.na), blk1 = (int)(nvb * (sp + 1) / a.grid.na);
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
@@ -396,7 +434,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
 #pragma unroll
     for (int q = 1; q < 4; ++q) o = stat_merge(o, sh[q * LP_BB + r]);
     if (in.b0 + r < a.rows)
-      a.part[(b * a.grid.splits + sp) * a.rows + in.b0 + r] = make_float4(o.m, o.s, o.t, 0.f);
+      a.part[(b * a.grid.na + sp) * a.rows + in.b0 + r] = make_float4(o.m, o.s, o.t, 0.f);
   }
 }
 
@@ -628,6 +666,7 @@ struct DzArgs {
   float scale;
   uint16_t *dz, *dzt;  // [nb, M, Vp], [nb, Vp, Mp]
   int64_t Vp, Mp;
+  Raster grid;
 };
 
 // dz of 256 positions by 256 table rows, rounded to 16 bits, and its transpose: the
@@ -637,7 +676,9 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   using Z = NtSize<2, BIAS>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   static_assert(Z::SMEM >= 256 * 512, "the tile fits the stages");
-  const int64_t b = blockIdx.z;
+  int ab, bb;
+  int64_t b;
+  if (!raster_place(a.grid, blockIdx.x, ab, bb, b)) return;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   NtIn in;
   in.A = a.W + b * a.ws;
@@ -646,8 +687,8 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   in.lda = in.ldb = a.ld;
   in.nA = a.v0 + a.nv;
   in.nB = (int)a.M;
-  in.a0 = a.v0 + blockIdx.y * 256;
-  in.b0 = blockIdx.x * LP_BB;
+  in.a0 = a.v0 + ab * 256;
+  in.b0 = bb * LP_BB;
   in.c0 = 0;
   in.c1 = a.chunks;
   in.nblk = 1;
@@ -754,6 +795,7 @@ struct OutArgs {
   const float* gsmax;   // times gsmax[b], if given
   uint16_t* out;
   float* f32;          // part [nb, splits, R, D] or acc [R, D]
+  Raster grid;         // instances: the shares of each
 };
 
 __device__ __forceinline__ float out_factor(float f, const RowGrad* rows, const float* gsmax,
@@ -767,9 +809,11 @@ template <int DT, int TCW>
 __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   using Z = NtSize<TCW, false>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
-  const int ndb = (a.D + Z::BA - 1) / Z::BA;
-  const int64_t b = blockIdx.z;
-  const int sp = blockIdx.y;
+  int ab, bb;
+  int64_t inst;
+  if (!raster_place(a.grid, blockIdx.x, ab, bb, inst)) return;
+  const int64_t b = inst / a.splits;
+  const int sp = (int)(inst % a.splits);
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   NtIn in;
   in.A = a.At + b * a.as;
@@ -778,8 +822,8 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   in.lda = in.ldb = a.ld;
   in.nA = a.D;
   in.nB = (int)a.R;
-  in.a0 = (blockIdx.x % ndb) * Z::BA;
-  in.b0 = (blockIdx.x / ndb) * LP_BB;
+  in.a0 = ab * Z::BA;
+  in.b0 = bb * LP_BB;
   in.c0 = sp * a.per * 4;
   in.c1 = min(a.chunks, in.c0 + a.per * 4);
   in.nblk = 1;
@@ -867,14 +911,14 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
     q.V = (int)a.V;
     q.chunks = (int)(w.Dk / 8);
     q.scale = a.scale;
-    q.grid = ScoreGrid{(int)((rows + LP_BB - 1) / LP_BB), w.plan.splits};
+    q.grid = make_raster(w.plan.splits, (rows + LP_BB - 1) / LP_BB, a.B);
     q.part = w.part;
     q.zt = w.zt;
     q.z = w.z;
     q.gmax = w.gmax;
     q.ldz = w.ldz;
     q.groups = w.groups;
-    const dim3 grid(score_blocks(q.grid), (unsigned)a.B);
+    const dim3 grid((unsigned)q.grid.blocks());
     if (a.bias) {
       if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
       else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
@@ -915,8 +959,8 @@ hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
   const int ba = narrow ? 128 : 256, nst = (q.chunks + 3) / 4;
   q.per = (nst + splits - 1) / splits;
   q.splits = (nst + q.per - 1) / q.per;
-  const dim3 grid((unsigned)((q.D + ba - 1) / ba * ((q.R + LP_BB - 1) / LP_BB)), (unsigned)q.splits,
-                  (unsigned)nb);
+  q.grid = make_raster((q.D + ba - 1) / ba, (q.R + LP_BB - 1) / LP_BB, nb * q.splits);
+  const dim3 grid((unsigned)q.grid.blocks());
   if (narrow) out_kernel<DT, 1><<<grid, NT_T, 0, s>>>(q);
   else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(q);
   hipError_t e = hipGetLastError();
@@ -978,7 +1022,8 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       d.dzt = (uint16_t*)w.dzt;
       d.Vp = vp;
       d.Mp = w.Mp;
-      const dim3 grid((unsigned)((a.M + LP_BB - 1) / LP_BB), (unsigned)((nv + 255) / 256), (unsigned)nb);
+      d.grid = make_raster((nv + 255) / 256, (a.M + LP_BB - 1) / LP_BB, nb);
+      const dim3 grid((unsigned)d.grid.blocks());
       if (a.bias) dz_kernel<DT, true><<<grid, NT_T, 0, s>>>(d);
       else dz_kernel<DT, false><<<grid, NT_T, 0, s>>>(d);
       if ((e = hipGetLastError()) != hipSuccess) return e;

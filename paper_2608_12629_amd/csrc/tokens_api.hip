@@ -50,13 +50,13 @@ constexpr int64_t SCORE_WGS = 1024, OUT_WGS = 512;
 
 // Shares of the column blocks: the number with the least rounds of 256 workgroups
 // times what one takes, its blocks and about six stages of filling and emptying.
-// Multiples of 8 from 8 on, so that each XCD gets as many.
-int score_splits(int64_t wgs, int64_t nvb, int64_t stages) {
-  const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / wgs));
+int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
+  const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / (nmb * B)));
   int best = 1;
   double least = HUGE_VAL;
   for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
-    const double us = (double)cdiv(wgs * s, 256) * ((double)(cdiv(nvb, s) * stages) + 6);
+    const double us = (double)cdiv(make_raster(s, nmb, B).blocks(), 256) *
+                      ((double)(cdiv(nvb, s) * stages) + 6);
     if (us < least) least = us, best = (int)s;
   }
   return best;
@@ -71,7 +71,7 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
   w.plan.rows = M;
   if (k) w.plan.rows = std::min(M, std::max<int64_t>(LP_SCORE_BYTES / (B * w.ldz * 4) / 256, 1) * 256);
   const int64_t nmb = cdiv(w.plan.rows, LP_BB), wgs = nmb * B;
-  w.plan.splits = score_splits(wgs, w.ldz / 256, cdiv(w.Dk, LP_DC));
+  w.plan.splits = score_splits(nmb, B, w.ldz / 256, cdiv(w.Dk, LP_DC));
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   // B x splits x rows, for any number of shares that these or fewer rows would get

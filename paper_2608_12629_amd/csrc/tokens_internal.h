@@ -52,6 +52,29 @@ constexpr int LP_GROUP = 64;
 // within LP_SCORE_BYTES; column blocks of 256 are shared out over `splits`
 // workgroups a row block, whose softmax statistics are merged.
 constexpr int64_t LP_SCORE_BYTES = (int64_t)1 << 30;
+//
+// Workgroup ids go round-robin over the 8 XCDs.  Blocks of A by blocks of B (and
+// instances) are walked in super-tiles of ga x gb workgroups, each on one XCD, so
+// that the 32 resident there share both operands' stages through its L2: per stage
+// ga + gb blocks come from beyond it instead of up to 33.
+struct Raster {
+  int na, nb, ga, gb;  // blocks of A and B, and of a super-tile
+  int64_t supers;      // of all instances
+  int64_t blocks() const { return (supers + 7) / 8 * 8 * ga * gb; }  // of the grid
+};
+// 4 x 8 where there are as many, then smaller until the XCDs' loads differ by at
+// most an eighth.
+inline Raster make_raster(int64_t na, int64_t nb, int64_t inst) {
+  Raster r{(int)na, (int)nb, (int)(na < 4 ? na : 4), 0, 0};
+  r.gb = (int)(nb < 32 / r.ga ? nb : 32 / r.ga);
+  if (r.gb < 8) r.ga = (int)(na < 32 / r.gb ? na : 32 / r.gb);
+  for (;;) {
+    r.supers = (na + r.ga - 1) / r.ga * ((nb + r.gb - 1) / r.gb) * inst;
+    if (r.ga * r.gb == 1 || r.blocks() * 8 <= na * nb * inst * 9) return r;
+    if (r.ga > r.gb) r.ga = (r.ga + 1) / 2;
+    else r.gb = (r.gb + 1) / 2;
+  }
+}
 struct LogprobsPlan {
   int64_t rows;    // rows of a block (all of M for k = 0)
   int splits;      // shares of the column blocks, a workgroup each
