@@ -23,7 +23,7 @@ namespace fkm {
 namespace {
 
 constexpr int NT_T = 512;  // threads of a workgroup
-constexpr float LOG2E = 1.44269504088896340736f;
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 constexpr float NEG_INF = -__builtin_inff();
 
 __device__ const uint4 nt_zero = {0, 0, 0, 0};
@@ -334,56 +334,68 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
     zt[tp] = 0.f;
     tgt[tp] = a.target && r < a.rows ? a.target[b * a.ts + r] : -1;
   }
+  const float c2 = a.scale * LOG2E;
   auto epi = [&](f32x16(&acc)[4][2], int g, const float* bias) {
     const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
     const bool edge = v0 + 64 > a.V;
-    float bz[2][16];
-    if constexpr (BIAS) {
+    if (BIAS || edge) {  // the scores themselves, with the offsets, into acc
 #pragma unroll
       for (int tc = 0; tc < 2; ++tc)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
+          f32x4 x = {0, 0, 0, 0};
+          const int at = tc * 32 + 8 * q + 4 * h;
+          if constexpr (BIAS) x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + at);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) bz[tc][4 * q + r] = x[r];
+          for (int r = 0; r < 4; ++r) {
+            // a forbidden token's score is -inf, whatever its row holds
+            const bool off = (BIAS && x[r] == NEG_INF) || v0 + at + r >= a.V;
+#pragma unroll
+            for (int tp = 0; tp < 4; ++tp) {
+              const float z = __builtin_fmaf(acc[tp][tc][4 * q + r], a.scale, x[r]);
+              acc[tp][tc][4 * q + r] = off ? NEG_INF : z;
+            }
+          }
         }
     }
+    const float zs = BIAS || edge ? 1.f : a.scale;  // acc to scores
 #pragma unroll
     for (int tp = 0; tp < 4; ++tp) {
-      float z[2][16], lm = -__FLT_MAX__;
+      float lm, es = 0.f, et = 0.f;
+      if (zs >= 0.f) {
+        float x = acc[tp][0][0];
 #pragma unroll
-      for (int tc = 0; tc < 2; ++tc)
+        for (int i = 1; i < 32; ++i) x = __builtin_fmaxf(x, acc[tp][i >> 4][i & 15]);
+        lm = x * zs;
+      } else {
+        float x = acc[tp][0][0];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          float x;
-          if constexpr (BIAS)  // a forbidden token's score is -inf, whatever its row holds
-            x = bz[tc][j] == NEG_INF ? NEG_INF : __builtin_fmaf(acc[tp][tc][j], a.scale, bz[tc][j]);
-          else
-            x = acc[tp][tc][j] * a.scale;
-          z[tc][j] = x;
-        }
-      if (edge) {
-#pragma unroll
-        for (int tc = 0; tc < 2; ++tc)
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (v0 + tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3) >= a.V) z[tc][j] = NEG_INF;
+        for (int i = 1; i < 32; ++i) x = __builtin_fminf(x, acc[tp][i >> 4][i & 15]);
+        lm = x * zs;
       }
-#pragma unroll
-      for (int tc = 0; tc < 2; ++tc)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) lm = __builtin_fmaxf(lm, z[tc][j]);
       if (lm > st[tp].m) stat_raise(st[tp], lm);
-      float es = 0.f, et = 0.f;
+      if (BIAS || edge) {  // in natural units: an offset may be the type's lowest value
 #pragma unroll
-      for (int tc = 0; tc < 2; ++tc)
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const float u = z[tc][j] - st[tp].m;
+        for (int i = 0; i < 32; ++i) {
+          const float u = acc[tp][i >> 4][i & 15] - st[tp].m;
           const float e = __builtin_amdgcn_exp2f(u * LOG2E);
           es += e;
           et = __builtin_fmaf(e, __builtin_fmaxf(u, -1e30f), et);  // 0 for -inf
         }
+      } else {
+        // in units of log 2, one fma: the vector ALU bounds this part, an exponential's
+        // four cycles for each of the others' one.  The maximum's product rounds by
+        // 2^-24 of it, as the scores themselves do.
+        const float m2 = st[tp].m * LOG2E;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+          const float u = __builtin_fmaf(acc[tp][i >> 4][i & 15], c2, -m2);
+          const float e = __builtin_amdgcn_exp2f(u);
+          es += e;
+          et = __builtin_fmaf(e, u, et);
+        }
+        et *= LN2;
+      }
       st[tp].s += es;
       st[tp].t += et;
       // the target, if it is among this lane's 32 columns
@@ -394,7 +406,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
         for (int tc = 0; tc < 2; ++tc)
 #pragma unroll
           for (int j = 0; j < 16; ++j)
-            if (hit && rel == tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3)) zt[tp] = z[tc][j];
+            if (hit && rel == tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3)) zt[tp] = acc[tp][tc][j] * zs;
       }
       if constexpr (TOPK) {
         const int64_t row = in.b0 + wp * 128 + tp * 32 + n;
@@ -405,9 +417,11 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
 #pragma unroll
           for (int tc = 0; tc < 2; ++tc)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q) {
+              const f32x16& x = acc[tp][tc];
               *reinterpret_cast<f32x4*>(zr + tc * 32 + 8 * q) =
-                  f32x4{z[tc][4 * q], z[tc][4 * q + 1], z[tc][4 * q + 2], z[tc][4 * q + 3]};
+                  f32x4{x[4 * q] * zs, x[4 * q + 1] * zs, x[4 * q + 2] * zs, x[4 * q + 3] * zs};
+            }
         }
       }
     }
@@ -614,12 +628,12 @@ __global__ __launch_bounds__(1024) void grad_gsmax_kernel(const RowGrad* __restr
   }
 }
 
-// in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance -> out [nb, C, ldo], zeros up to
-// ldo.  Rows that take no part become zeros: of X those without a gradient (the others
+// in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance -> out [nb, C, ldo], zeros up
+// to np.  Rows that take no part become zeros: of X those without a gradient (the others
 // times gs / gsmax for fp16), of W the forbidden tokens.
 template <int DT>
 __global__ __launch_bounds__(256) void transpose_kernel(
-    const uint16_t* __restrict__ in, int64_t R, int C, int64_t r0, int64_t nr, int64_t ldo,
+    const uint16_t* __restrict__ in, int64_t R, int C, int64_t r0, int64_t nr, int64_t np, int64_t ldo,
     const RowGrad* __restrict__ rows, const float* __restrict__ gsmax,
     const float* __restrict__ bias, uint16_t* __restrict__ out) {
   __shared__ uint16_t tile[64][66];
@@ -651,7 +665,7 @@ __global__ __launch_bounds__(256) void transpose_kernel(
   for (int i = t; i < 64 * 64; i += 256) {
     const int c = ct + i / 64;
     const int64_t r = rt + i % 64;
-    if (c < C && r < ldo) out[c * ldo + r] = tile[i % 64][i / 64];
+    if (c < C && r < np) out[c * ldo + r] = tile[i % 64][i / 64];
   }
 }
 
@@ -664,8 +678,8 @@ struct DzArgs {
   int V, v0, nv;    // all table rows; the block of them
   int chunks;
   float scale;
-  uint16_t *dz, *dzt;  // [nb, M, Vp], [nb, Vp, Mp]
-  int64_t Vp, Mp;
+  uint16_t *dz, *dzt;  // [nb, M, lv], [nb, Vp, lm], zeros up to Vp and Mp
+  int64_t Vp, Mp, lv, lm;
   Raster grid;
 };
 
@@ -751,13 +765,13 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   loop.run(epi);
 
   const int64_t vb = in.a0 - a.v0;  // within the block of table rows
-  uint16_t* dz = a.dz + b * a.M * a.Vp;
-  uint16_t* dzt = a.dzt + b * a.Vp * a.Mp;
+  uint16_t* dz = a.dz + b * a.M * a.lv;
+  uint16_t* dzt = a.dzt + b * a.Vp * a.lm;
 #pragma unroll 4
   for (int i = threadIdx.x; i < 256 * 32; i += NT_T) {
     const int rl = i >> 5, c = i & 31;
     if (in.b0 + rl < a.M && vb + 8 * c < a.Vp)
-      *reinterpret_cast<uint4*>(dz + (in.b0 + rl) * a.Vp + vb + 8 * c) = nt_at<uint4>(smem, at(rl, c));
+      *reinterpret_cast<uint4*>(dz + (in.b0 + rl) * a.lv + vb + 8 * c) = nt_at<uint4>(smem, at(rl, c));
   }
 #pragma unroll 2
   for (int i = threadIdx.x; i < 128 * 32; i += NT_T) {
@@ -772,9 +786,9 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
       lo[e] = (x[2 * e] & 0xffffu) | (x[2 * e + 1] << 16);
       hi[e] = (x[2 * e] >> 16) | (x[2 * e + 1] & 0xffff0000u);
     }
-    uint16_t* o = dzt + (vb + 2 * vp) * a.Mp + in.b0 + 8 * mo;
+    uint16_t* o = dzt + (vb + 2 * vp) * a.lm + in.b0 + 8 * mo;
     *reinterpret_cast<uint4*>(o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    *reinterpret_cast<uint4*>(o + a.Mp) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(o + a.lm) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
   }
 }
 
@@ -980,7 +994,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     X = (const char*)w.xpad;
     W = (const char*)w.wpad;
   }
-  const int64_t rows = a.B * a.M;
+  const int64_t rows = a.B * a.M, lm = grad_ld(w.Mp);
   grad_rows_kernel<DT><<<dim3((unsigned)std::min<int64_t>((rows + 255) / 256, 1 << 16)), 256, 0, s>>>(
       a.target, a.lse, a.entropy, a.g, a.h, a.bias, rows, a.M, (int)a.V, w.rows);
   if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -995,13 +1009,13 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     const float* gsmax = f16 ? w.gsmax + b0 : nullptr;
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
     transpose_kernel<DT><<<dim3((unsigned)(w.Mp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
-        (const uint16_t*)a.X + b0 * a.M * a.D, a.M, (int)a.D, 0, a.M, w.Mp, rg, gsmax, nullptr,
+        (const uint16_t*)a.X + b0 * a.M * a.D, a.M, (int)a.D, 0, a.M, w.Mp, lm, rg, gsmax, nullptr,
         (uint16_t*)w.xt);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
-      const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64;
+      const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
       transpose_kernel<DT><<<dim3((unsigned)(vp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
-          (const uint16_t*)a.W + b0 * a.V * a.D, a.V, (int)a.D, v0, nv, vp, nullptr, nullptr, bias,
+          (const uint16_t*)a.W + b0 * a.V * a.D, a.V, (int)a.D, v0, nv, vp, lv, nullptr, nullptr, bias,
           (uint16_t*)w.wt);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       DzArgs d;
@@ -1022,6 +1036,8 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       d.dzt = (uint16_t*)w.dzt;
       d.Vp = vp;
       d.Mp = w.Mp;
+      d.lv = lv;
+      d.lm = lm;
       d.grid = make_raster((nv + 255) / 256, (a.M + LP_BB - 1) / LP_BB, nb);
       const dim3 grid((unsigned)d.grid.blocks());
       if (a.bias) dz_kernel<DT, true><<<grid, NT_T, 0, s>>>(d);
@@ -1034,7 +1050,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       // dX: positions by D, over the table rows of this block
       q.At = (const char*)w.wt;
       q.Br = (const char*)w.dz;
-      q.ld = vp * 2;
+      q.ld = lv * 2;
       q.as = a.D * q.ld;
       q.bs = a.M * q.ld;
       q.R = q.os = a.M;
@@ -1048,7 +1064,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       // dW: the block's table rows by D, over the positions
       q.At = (const char*)w.xt;
       q.Br = (const char*)w.dzt;
-      q.ld = w.Mp * 2;
+      q.ld = lm * 2;
       q.as = a.D * q.ld;
       q.bs = vp * q.ld;
       q.R = nv;

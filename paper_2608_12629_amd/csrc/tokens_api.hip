@@ -107,11 +107,13 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   take(w.rows, (size_t)(B * M) * sizeof(RowGrad));
   take(w.gsmax, (size_t)B * 4);
   // sizes that never shrink as M grows, whatever the plan then is
-  const size_t dz = (size_t)std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2);
+  // (and 64 more elements a row: grad_ld)
+  const size_t dz = (size_t)(std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2) +
+                             B * std::max(w.Mp, Vall) * 64 * 2);
   take(w.dz, dz);
   take(w.dzt, dz);
-  take(w.xt, (size_t)(B * D * w.Mp) * 2);
-  take(w.wt, (size_t)(B * D * Vall) * 2);
+  take(w.xt, (size_t)(B * D * (w.Mp + 64)) * 2);
+  take(w.wt, (size_t)(B * D * (Vall + 64)) * 2);
   take(w.accx, w.Vc < V ? (size_t)(M * D) * 4 : 0);
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
   const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);

@@ -114,12 +114,15 @@ struct RowGrad {  // one position
   float gs;       // a power of two: what dz of this row is divided by (fp16; else 1)
   int pad;
 };
+// Elements from row to row of dz and the copies: 128 bytes past a multiple of 1 KiB, so
+// that a stage's 64 bytes of each of 512 rows do not all lie in one L2 channel.
+inline int64_t grad_ld(int64_t n) { return n % 512 == 0 ? n + 64 : n; }
 struct GradWs {
   void *xpad, *wpad;
   RowGrad* rows;    // [B, M]
   float* gsmax;     // [B] largest gs
-  void *dz, *dzt;   // [nb, M, Vp], [nb, Vp, Mp]
-  void *xt, *wt;    // [nb, D, Mp], [nb, D, Vp]
+  void *dz, *dzt;   // [nb, M, grad_ld(Vp)], [nb, Vp, grad_ld(Mp)]
+  void *xt, *wt;    // [nb, D, grad_ld(Mp)], [nb, D, grad_ld(Vp)]
   float* accx;      // [M, D] dX over the blocks of table rows, where there are several
   float* part;      // [nb, splits, rows, D] shares of a contraction
   int64_t Dk, Mp, Vp, Vc;
