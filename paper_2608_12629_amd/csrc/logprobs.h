@@ -412,7 +412,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
         const int64_t row = in.b0 + wp * 128 + tp * 32 + n;
         const float gm = __builtin_fmaxf(lm, __shfl_xor(lm, 32));
         if (row < a.rows) {
-          if (h == 0) a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = gm;
+          if (h == 0 && v0 < a.V) a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = gm;
           float* zr = a.z + (b * a.rows + row) * a.ldz + v0 + 4 * h;
 #pragma unroll
           for (int tc = 0; tc < 2; ++tc)
@@ -452,6 +452,131 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   }
 }
 
+// ---- few rows --------------------------------------------------------------------
+// Up to 64 rows (a decoding step): the table streams through once, bound by HBM.  A
+// workgroup owns 64 table rows and all positions; its four waves split the contraction
+// in units of 64 elements (whole 128-byte lines of each row), each wave holding 4 x CB
+// 16 x 16 x 32 MFMA tiles and loading the fragments of both operands straight into
+// registers, two units ahead, without LDS or barriers.  The waves' sums meet in LDS,
+// where each wave then has the 64 scores of a position in its lanes.  131,072 x 4,096
+// bf16: one row 264 -> 186 us (5.8 TB/s), against the tiles of 256 positions.
+struct FewArgs {
+  const char *X, *W;
+  const float* bias;
+  const int32_t* target;
+  int M, V, chunks;
+  int64_t ld;  // bytes of a row
+  float scale;
+  float4* part;  // [B, blocks, M]
+  float* zt;     // [B, M]
+  float *z, *gmax;
+  int64_t ldz, groups;
+};
+
+template <int DT, int CB, bool BIAS, bool TOPK>
+__global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
+  constexpr int LDR = 68;  // floats from position to position: 64 scores and 4 of padding
+  __shared__ __attribute__((aligned(16))) float red[4][16 * CB * LDR];
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t b = blockIdx.y;
+  const int v0 = blockIdx.x * 64;
+  const char *pa[4], *pb[CB];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    pa[i] = a.W + (b * a.V + min(v0 + 16 * i + r16, a.V - 1)) * a.ld + q4 * 16;
+#pragma unroll
+  for (int i = 0; i < CB; ++i) pb[i] = a.X + (b * a.M + min(16 * i + r16, a.M - 1)) * a.ld + q4 * 16;
+  struct Unit {
+    uint4 a[2][4], b[2][CB];
+  };
+  auto fetch = [&](Unit& f, int u) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        f.a[st][i] = *reinterpret_cast<const uint4*>(pa[i] + (int64_t)u * 128 + st * 64);
+#pragma unroll
+      for (int i = 0; i < CB; ++i)
+        f.b[st][i] = *reinterpret_cast<const uint4*>(pb[i] + (int64_t)u * 128 + st * 64);
+    }
+  };
+  f32x4 acc[4][CB];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < CB; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+  auto mfma = [&](const Unit& f) {
+#pragma unroll
+    for (int st = 0; st < 2; ++st)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < CB; ++j) acc[i][j] = mfma_chunk<DT>(f.a[st][i], f.b[st][j], acc[i][j]);
+  };
+  const int full = a.chunks / 8;  // whole units; then one with what is left
+  Unit f0, f1;
+  int u = w;
+  if (u < full) fetch(f0, u);
+  if (u + 4 < full) fetch(f1, u + 4);
+  for (; u + 4 < full; u += 8) {
+    mfma(f0);
+    if (u + 8 < full) fetch(f0, u + 8);
+    mfma(f1);
+    if (u + 12 < full) fetch(f1, u + 12);
+  }
+  if (u < full) mfma(f0);
+  if (full * 8 < a.chunks && w == full % 4) {
+    Unit f;
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+      const bool in = full * 8 + st * 4 + q4 < a.chunks;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        f.a[st][i] = in ? *reinterpret_cast<const uint4*>(pa[i] + (int64_t)full * 128 + st * 64)
+                        : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int i = 0; i < CB; ++i)
+        f.b[st][i] = in ? *reinterpret_cast<const uint4*>(pb[i] + (int64_t)full * 128 + st * 64)
+                        : make_uint4(0, 0, 0, 0);
+    }
+    mfma(f);
+  }
+  // lane 16 q + c holds rows 4 q .. 4 q + 3 of column c
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < CB; ++j)
+      *reinterpret_cast<f32x4*>(&red[w][(16 * j + r16) * LDR + 16 * i + 4 * q4]) = acc[i][j];
+  __syncthreads();
+  const int v = v0 + lane;
+  const float bz = BIAS && v < a.V ? a.bias[b * a.V + v] : 0.f;
+  const bool off = v >= a.V || (BIAS && bz == NEG_INF);
+  for (int m = w; m < a.M; m += 4) {
+    const int at = m * LDR + lane;
+    const float x = (red[0][at] + red[1][at]) + (red[2][at] + red[3][at]);
+    const float z = off ? NEG_INF : __builtin_fmaf(x, a.scale, bz);
+    float lm = z;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) lm = __builtin_fmaxf(lm, __shfl_xor(lm, d));
+    const float mx = __builtin_fmaxf(lm, -__FLT_MAX__);
+    const float un = z - mx;
+    float s = __builtin_amdgcn_exp2f(un * LOG2E), t = s * __builtin_fmaxf(un, -1e30f);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      s += __shfl_xor(s, d);
+      t += __shfl_xor(t, d);
+    }
+    if (lane == 0) a.part[(b * gridDim.x + blockIdx.x) * a.M + m] = make_float4(mx, s, t, 0.f);
+    if (a.target && v < a.V && a.target[b * a.M + m] == v) a.zt[b * a.M + m] = z;
+    if constexpr (TOPK) {
+      if (lane == 0) a.gmax[(b * a.M + m) * a.groups + blockIdx.x] = lm;
+      a.z[(b * a.M + m) * a.ldz + v] = z;
+    }
+  }
+}
+
+// ---- results of a row --------------------------------------------------------------
 // Scores as integers in the same order (-0 as +0).
 __device__ __forceinline__ uint32_t score_key(float v) {
   const uint32_t u = __float_as_uint(v + 0.f);
@@ -473,15 +598,50 @@ struct FinishArgs {
   float* top_logprob;
 };
 
-// One wave per row: the shares' statistics merged, and the k best: the k groups of
-// the largest best scores (ties to the lowest group) hold them, since each of these
-// has an entry as good as anything elsewhere; then k times the best of their entries.
-template <bool TOPK>
-__global__ __launch_bounds__(64) void logprobs_finish_kernel(FinishArgs a) {
-  const int64_t row = blockIdx.x, b = blockIdx.y;
-  const int lane = threadIdx.x;
+__device__ __forceinline__ void finish_row(const FinishArgs& a, int64_t b, int64_t row, const Stat& st,
+                                           float logs) {
+  const bool none = st.s == 0.f;  // every token is forbidden
+  const int64_t o = b * a.ts + row;
+  a.lse[o] = none ? NEG_INF : st.m + logs;
+  if (a.entropy) a.entropy[o] = none ? 0.f : logs - st.t / st.s;
+  if (a.target) {
+    const int t = a.target[o];
+    a.logprob[o] = (unsigned)t >= (unsigned)a.V ? 0.f
+                   : none ? NEG_INF : (a.zt[b * a.rows + row] - st.m) - logs;
+  }
+}
+
+// One thread per row: a few shares' statistics merged in order.
+__global__ __launch_bounds__(256) void finish_rows_kernel(FinishArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
+  if (row >= a.rows) return;
   Stat st = stat_none();
-  for (int sp = lane; sp < a.splits; sp += 64) {
+  for (int sp = 0; sp < a.splits; ++sp) {
+    const float4 p = a.part[(b * a.splits + sp) * a.rows + row];
+    st = stat_merge(st, Stat{p.x, p.y, p.z});
+  }
+  finish_row(a, b, row, st, logf(st.s));
+}
+
+// One workgroup per row: many shares, and the k best.
+//
+// The k best lie in groups whose best score is among the k largest of those (ties to the
+// lowest group): each of these groups has an entry as good as anything elsewhere.  Every
+// thread keeps the best of its groups; the k-th largest of the 256 thread bests is a
+// bound that k groups reach, few others do, and nothing below it is among the k best.
+// The entries that reach it, gathered from those groups, are ranked against each other.
+// Where too many reach it (equal scores, a large table's best tokens in one thread), the
+// bound is raised to the k-th largest group best, which the lowest groups that reach it
+// settle exactly, and the entries are taken one by one.
+constexpr int TOP_GROUPS = 64, TOP_ENTRIES = 256;
+
+template <bool TOPK>
+__global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
+  const int64_t row = blockIdx.x, b = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  __shared__ Stat sh[4];
+  Stat st = stat_none();
+  for (int sp = tid; sp < a.splits; sp += 256) {
     const float4 p = a.part[(b * a.splits + sp) * a.rows + row];
     st = stat_merge(st, Stat{p.x, p.y, p.z});
   }
@@ -490,66 +650,137 @@ __global__ __launch_bounds__(64) void logprobs_finish_kernel(FinishArgs a) {
     const Stat o = {__shfl_xor(st.m, m), __shfl_xor(st.s, m), __shfl_xor(st.t, m)};
     st = stat_merge(lane & m ? o : st, lane & m ? st : o);
   }
-  const bool none = st.s == 0.f;  // every token is forbidden
-  const float logs = logf(st.s), lse = none ? NEG_INF : st.m + logs;
-  if (lane == 0) {
-    const int64_t o = b * a.ts + row;
-    a.lse[o] = lse;
-    if (a.entropy) a.entropy[o] = none ? 0.f : logs - st.t / st.s;
-    if (a.target) {
-      const int t = a.target[o];
-      a.logprob[o] = (unsigned)t >= (unsigned)a.V ? 0.f
-                     : none ? NEG_INF : (a.zt[b * a.rows + row] - st.m) - logs;
-    }
-  }
+  if (lane == 0) sh[w] = st;
+  __syncthreads();
+  st = stat_merge(stat_merge(sh[0], sh[1]), stat_merge(sh[2], sh[3]));
+  const float logs = logf(st.s);
+  if (tid == 0) finish_row(a, b, row, st, logs);
   if constexpr (TOPK) {
-    extern __shared__ uint32_t gk[];  // keys of the groups' best scores
-    __shared__ int sel[TOK_MAX_K];
+    __shared__ uint32_t best[256], ekey[TOP_ENTRIES];
+    __shared__ int eidx[TOP_ENTRIES], sel[TOP_GROUPS];
+    __shared__ uint32_t bound_s;
+    __shared__ int ngroups, nentries, cnt_s[4];
     const float* gm = a.gmax + (b * a.rows + row) * a.groups;
+    const float* zr = a.z + (b * a.rows + row) * a.ldz;
     const int G = (int)a.groups, k = a.k, kg = min(k, G);
-    for (int i = lane; i < G; i += 64) gk[i] = score_key(gm[i]);
+    int32_t* ti = a.top_idx + (b * a.ts + row) * k;
+    float* tl = a.top_logprob + (b * a.ts + row) * k;
+    const bool none = st.s == 0.f;
+    auto put = [&](int j, uint32_t key, int v) {  // forbidden tokens are no alternatives
+      const bool have = key > score_key(NEG_INF) && v < a.V && !none;
+      ti[j] = have ? v : -1;
+      tl[j] = have ? (key_score(key) - st.m) - logs : NEG_INF;
+    };
+    // with few groups (a table of up to 4,096 rows) the entries themselves
+    const bool direct = G <= TOP_GROUPS;
+    uint32_t mine = 0;
+    if (direct)
+      for (int i = tid; i < a.V; i += 256) mine = max(mine, score_key(zr[i]));
+    else
+      for (int i = tid; i < G; i += 256) mine = max(mine, score_key(gm[i]));
+    best[tid] = mine;
+    if (tid == 0) ngroups = nentries = 0;
     __syncthreads();
-    uint32_t kth = 0;  // the kg-th largest: the largest value that kg groups reach
+    if (w == 0) {  // the k-th largest of the thread bests
+      uint32_t x[4], kth = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = best[lane + 64 * i];
+      for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t c = kth | (1u << bit);
+        int cnt = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cnt += __popcll(__ballot(x[i] >= c));
+        if (cnt >= k) kth = c;
+        if (cnt == k) break;  // exactly k reach it: bound enough
+      }
+      if (lane == 0) bound_s = kth;
+    }
+    __syncthreads();
+    const uint32_t bound = bound_s;
+    auto entry = [&](int v) {
+      const uint32_t key = score_key(zr[v]);
+      if (key >= bound) {
+        const int at = atomicAdd(&nentries, 1);
+        if (at < TOP_ENTRIES) ekey[at] = key, eidx[at] = v;
+      }
+    };
+    if (direct) {
+      for (int v = tid; v < a.V; v += 256) entry(v);
+    } else {
+      for (int i = tid; i < G; i += 256)
+        if (score_key(gm[i]) >= bound) {
+          const int at = atomicAdd(&ngroups, 1);
+          if (at < TOP_GROUPS) sel[at] = i;
+        }
+      __syncthreads();
+      const int ng = ngroups;
+      if (ng > TOP_GROUPS) {
+        if (tid == 0) nentries = TOP_ENTRIES + 1;
+      } else {
+        for (int i = w; i < ng; i += 4) entry(sel[i] * LP_GROUP + lane);
+      }
+    }
+    __syncthreads();
+    const int n = nentries;  // at least k
+    if (n <= TOP_ENTRIES) {
+      // each entry's rank: whichever way they were gathered, the order is the same
+      if (tid < n) {
+        const uint32_t key = ekey[tid];
+        const int v = eidx[tid];
+        int rank = 0;
+        for (int i = 0; i < n; ++i) {
+          const uint32_t o = ekey[i];
+          rank += o > key || (o == key && eidx[i] < v) ? 1 : 0;
+        }
+        if (rank < k) put(rank, key, v);
+      }
+      return;
+    }
+    // exactly: the kg-th largest group best, then the lowest groups that reach it
+    auto count = [&](uint32_t c, bool over) {  // groups whose best reaches (exceeds) c
+      int n = 0;
+      for (int i = tid; i < G; i += 256) {
+        const uint32_t key = score_key(gm[i]);
+        n += over ? key > c : key >= c;
+      }
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) n += __shfl_xor(n, m);
+      __syncthreads();
+      if (lane == 0) cnt_s[w] = n;
+      __syncthreads();
+      return cnt_s[0] + cnt_s[1] + cnt_s[2] + cnt_s[3];
+    };
+    uint32_t kth = 0;
     for (int bit = 31; bit >= 0; --bit) {
       const uint32_t c = kth | (1u << bit);
-      int cnt = 0;
-      for (int i = lane; i < G; i += 64) cnt += gk[i] >= c ? 1 : 0;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) cnt += __shfl_xor(cnt, m);
-      if (cnt >= kg) kth = c;
+      if (count(c, false) >= kg) kth = c;
     }
-    int above = 0;
-    for (int i = lane; i < G; i += 64) above += gk[i] > kth ? 1 : 0;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) above += __shfl_xor(above, m);
-    int ties = kg - above, got = 0;  // groups at kth itself to take, lowest first
+    int ties = kg - count(kth, true), got = 0;
+    __syncthreads();
+    if (w != 0) return;
     for (int i0 = 0; i0 < G && got < kg; i0 += 64) {
-      const int i = i0 + lane;
-      const uint32_t key = i < G ? gk[i] : 0u;
-      const bool over = i < G && key > kth, tie = i < G && key == kth;
-      const uint64_t tm = __ballot(tie);
-      const uint64_t below = (1ull << lane) - 1;
-      const bool take = over || (tie && __popcll(tm & below) < ties);
+      const uint32_t key = i0 + lane < G ? score_key(gm[i0 + lane]) : 0u;
+      const bool in = i0 + lane < G, tie = in && key == kth;
+      const uint64_t tm = __ballot(tie), below = (1ull << lane) - 1;
+      const bool take = (in && key > kth) || (tie && __popcll(tm & below) < ties);
       const uint64_t km = __ballot(take);
-      if (take) sel[got + __popcll(km & below)] = i;
+      if (take) sel[got + __popcll(km & below)] = i0 + lane;
       got += __popcll(km);
       ties -= min(ties, (int)__popcll(tm));
     }
-    __syncthreads();
-    // entry `lane` of each chosen group; groups in ascending order
-    const float* zr = a.z + (b * a.rows + row) * a.ldz;
-    uint32_t key[TOK_MAX_K];
+    __builtin_amdgcn_wave_barrier();
+    uint32_t key[TOK_MAX_K];  // entry `lane` of each chosen group; groups in ascending order
 #pragma unroll
     for (int i = 0; i < TOK_MAX_K; ++i)
       key[i] = i < kg ? score_key(zr[(int64_t)sel[i] * LP_GROUP + lane]) : 0u;
     for (int j = 0; j < k; ++j) {
-      uint32_t best = 0;
+      uint32_t top = 0;
       int at = -1;
 #pragma unroll
       for (int i = 0; i < TOK_MAX_K; ++i)
-        if (key[i] > best) best = key[i], at = i;
-      int v = at >= 0 ? sel[at] * LP_GROUP + lane : 0x7fffffff;
-      uint32_t wb = best;
+        if (key[i] > top) top = key[i], at = i;
+      const int v = at >= 0 ? sel[at] * LP_GROUP + lane : 0x7fffffff;
+      uint32_t wb = top;
       int wv = v;
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) {
@@ -562,13 +793,7 @@ __global__ __launch_bounds__(64) void logprobs_finish_kernel(FinishArgs a) {
         for (int i = 0; i < TOK_MAX_K; ++i)
           if (i == at) key[i] = 0u;
       }
-      if (lane == 0) {
-        const float zb = key_score(wb);
-        const bool have = wb > score_key(NEG_INF) && wv < a.V && !none;
-        const int64_t o = (b * a.ts + row) * k + j;
-        a.top_idx[o] = have ? wv : -1;
-        a.top_logprob[o] = have ? (zb - st.m) - logs : NEG_INF;
-      }
+      if (lane == 0) put(j, wb, wv);
     }
   }
 }
@@ -900,6 +1125,19 @@ __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs a, int64_t nb) 
 }
 
 // ---- launchers -------------------------------------------------------------------
+template <int DT, int CB>
+hipError_t launch_few(const FewArgs& q, const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s) {
+  const dim3 grid((unsigned)w.plan.splits, (unsigned)a.B);
+  if (a.bias) {
+    if (a.k) few_kernel<DT, CB, true, true><<<grid, 256, 0, s>>>(q);
+    else few_kernel<DT, CB, true, false><<<grid, 256, 0, s>>>(q);
+  } else {
+    if (a.k) few_kernel<DT, CB, false, true><<<grid, 256, 0, s>>>(q);
+    else few_kernel<DT, CB, false, false><<<grid, 256, 0, s>>>(q);
+  }
+  return hipGetLastError();
+}
+
 template <int DT>
 hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s) {
   hipError_t e;
@@ -912,41 +1150,50 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
   }
   for (int64_t m0 = 0; m0 < a.M; m0 += w.plan.rows) {
     const int64_t rows = std::min(w.plan.rows, a.M - m0);
-    ScoreArgs q;
-    q.X = X + m0 * w.Dk * 2;
-    q.W = W;
-    q.bias = a.bias;
-    q.target = a.target ? a.target + m0 : nullptr;
-    q.xs = a.M * w.Dk * 2;
-    q.ws = a.V * w.Dk * 2;
-    q.ts = a.M;
-    q.rows = rows;
-    q.ld = w.Dk * 2;
-    q.V = (int)a.V;
-    q.chunks = (int)(w.Dk / 8);
-    q.scale = a.scale;
-    q.grid = make_raster(w.plan.splits, (rows + LP_BB - 1) / LP_BB, a.B);
-    q.part = w.part;
-    q.zt = w.zt;
-    q.z = w.z;
-    q.gmax = w.gmax;
-    q.ldz = w.ldz;
-    q.groups = w.groups;
-    const dim3 grid((unsigned)q.grid.blocks());
-    if (a.bias) {
-      if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
-      else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
+    if (w.plan.few) {
+      const FewArgs q{X, W, a.bias, a.target, (int)a.M, (int)a.V, (int)(w.Dk / 8), w.Dk * 2, a.scale,
+                      w.part, w.zt, w.z, w.gmax, w.ldz, w.groups};
+      const int cb = (int)((a.M + 15) / 16);
+      e = cb == 1 ? launch_few<DT, 1>(q, a, w, s) : cb == 2 ? launch_few<DT, 2>(q, a, w, s)
+                                                            : launch_few<DT, 4>(q, a, w, s);
     } else {
-      if (a.k) score_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(q);
-      else score_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(q);
+      ScoreArgs q;
+      q.X = X + m0 * w.Dk * 2;
+      q.W = W;
+      q.bias = a.bias;
+      q.target = a.target ? a.target + m0 : nullptr;
+      q.xs = a.M * w.Dk * 2;
+      q.ws = a.V * w.Dk * 2;
+      q.ts = a.M;
+      q.rows = rows;
+      q.ld = w.Dk * 2;
+      q.V = (int)a.V;
+      q.chunks = (int)(w.Dk / 8);
+      q.scale = a.scale;
+      q.grid = make_raster(w.plan.splits, (rows + LP_BB - 1) / LP_BB, a.B);
+      q.part = w.part;
+      q.zt = w.zt;
+      q.z = w.z;
+      q.gmax = w.gmax;
+      q.ldz = w.ldz;
+      q.groups = w.groups;
+      const dim3 grid((unsigned)q.grid.blocks());
+      if (a.bias) {
+        if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
+        else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
+      } else {
+        if (a.k) score_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(q);
+        else score_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(q);
+      }
+      e = hipGetLastError();
     }
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (e != hipSuccess) return e;
     FinishArgs f;
     f.part = w.part;
     f.zt = w.zt;
     f.z = w.z;
     f.gmax = w.gmax;
-    f.target = q.target;
+    f.target = a.target ? a.target + m0 : nullptr;
     f.rows = rows;
     f.ts = a.M;
     f.ldz = w.ldz;
@@ -959,9 +1206,12 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
     f.lse = a.lse + m0;
     f.top_idx = a.top_idx + m0 * a.k;
     f.top_logprob = a.top_logprob + m0 * a.k;
-    const dim3 fgrid((unsigned)rows, (unsigned)a.B);
-    if (a.k) logprobs_finish_kernel<true><<<fgrid, 64, w.groups * 4, s>>>(f);
-    else logprobs_finish_kernel<false><<<fgrid, 64, 0, s>>>(f);
+    // a thread merges a few shares in a row; a workgroup many
+    if (a.k) finish_top_kernel<true><<<dim3((unsigned)rows, (unsigned)a.B), 256, 0, s>>>(f);
+    else if (f.splits > 32)
+      finish_top_kernel<false><<<dim3((unsigned)rows, (unsigned)a.B), 256, 0, s>>>(f);
+    else
+      finish_rows_kernel<<<dim3((unsigned)((rows + 255) / 256), (unsigned)a.B), 256, 0, s>>>(f);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   return hipSuccess;

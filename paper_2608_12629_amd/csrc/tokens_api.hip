@@ -67,15 +67,17 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
   Taker take{(char*)base};
   w.Dk = up(D, 8);
   w.ldz = up(V, 256);
-  w.groups = w.ldz / LP_GROUP;
+  w.groups = cdiv(V, LP_GROUP);
   w.plan.rows = M;
   if (k) w.plan.rows = std::min(M, std::max<int64_t>(LP_SCORE_BYTES / (B * w.ldz * 4) / 256, 1) * 256);
   const int64_t nmb = cdiv(w.plan.rows, LP_BB), wgs = nmb * B;
-  w.plan.splits = score_splits(nmb, B, w.ldz / 256, cdiv(w.Dk, LP_DC));
+  w.plan.few = M <= LP_FEW_M;
+  w.plan.splits = w.plan.few ? (int)cdiv(V, 64) : score_splits(nmb, B, w.ldz / 256, cdiv(w.Dk, LP_DC));
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   // B x splits x rows, for any number of shares that these or fewer rows would get
-  take(w.part, (size_t)(std::max(SCORE_WGS, wgs) * LP_BB) * sizeof(float4));
+  take(w.part, (size_t)std::max(std::max(SCORE_WGS, wgs) * LP_BB,
+                                B * std::min(M, LP_FEW_M) * cdiv(V, 64)) * sizeof(float4));
   take(w.zt, (size_t)(B * w.plan.rows) * 4);
   take(w.gmax, k ? (size_t)(B * w.plan.rows * w.groups) * 4 : 0);
   take(w.z, k ? (size_t)(B * w.plan.rows * w.ldz) * 4 : 0);

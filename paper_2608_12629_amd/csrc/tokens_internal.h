@@ -75,9 +75,11 @@ inline Raster make_raster(int64_t na, int64_t nb, int64_t inst) {
     else r.gb = (r.gb + 1) / 2;
   }
 }
+constexpr int64_t LP_FEW_M = 64;
 struct LogprobsPlan {
   int64_t rows;    // rows of a block (all of M for k = 0)
-  int splits;      // shares of the column blocks, a workgroup each
+  bool few;        // up to LP_FEW_M rows: a workgroup for every 64 columns and all rows
+  int splits;      // shares of the columns, a workgroup each
 };
 struct LogprobsWs {
   void *xpad, *wpad;  // rows of Dk elements, where D is no multiple of 8
