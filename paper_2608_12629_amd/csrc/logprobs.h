@@ -209,18 +209,25 @@ struct NtLoop {
   // stage s + 1's first fragments and start stage s + 3 into the buffer of stage s - 1,
   // which every wave has finished.  Past the last stage the reads bring values that
   // nobody uses; one path for all stages keeps the accumulators in their registers.
-  __device__ __forceinline__ void stage(int s, int S, f32x16 (&acc)[4][TCW], NtFrag<TCW>& f0,
-                                        NtFrag<TCW>& f1) {
+  // `landed`: this wave knows that the loads of stage s + 1 are done.
+  __device__ __forceinline__ void stage(int s, int S, bool landed, f32x16 (&acc)[4][TCW],
+                                        NtFrag<TCW>& f0, NtFrag<TCW>& f1) {
     step<false>(acc, f0, f1, at(s), loff1, nullptr, false);
-    // (vmcnt counts in issue order: an epilogue's stores only make the wait longer)
-    if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
+    if (landed) nt_wait_and_sync<63>();
+    else if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
     else nt_wait_and_sync<0>();
     step<true>(acc, f1, f0, at(s + 1), loff0, at(s + 3), s + 3 < S);
   }
   __device__ __forceinline__ char* at(int s) { return smem + (s & 3) * Z::STAGE; }
 
-  // epi(acc, block, bias of the block in LDS) after each block
-  template <class Epi>
+  // epi(acc, block, the finished stage's buffer) after each block.  Every wave is past
+  // that stage's barrier, and so has read it; nothing is loaded into it before the next
+  // stage's barrier, which every wave reaches after its epilogue: it is free, but for the
+  // block's bias behind the operands.  STORES: the epilogue waits for the loads in flight
+  // (of the next three stages) before its first store, so that the stages after it need
+  // not: vmcnt counts in issue order, and a wait for loads that were issued after stores
+  // waits for the stores.
+  template <bool STORES, class Epi>
   __device__ __forceinline__ void run(Epi&& epi) {
     const int S = in.nblk * nds;
     issue(at(0));
@@ -232,7 +239,7 @@ struct NtLoop {
     NtFrag<TCW> f0, f1;
     read(f0, at(0), loff0);
     f32x16 acc[4][TCW];
-    int s = 0;
+    int s = 0, landed = 0;
     for (int g = 0; g < in.nblk; ++g) {
 #pragma unroll
       for (int tp = 0; tp < 4; ++tp)
@@ -240,8 +247,9 @@ struct NtLoop {
         for (int tc = 0; tc < TCW; ++tc)
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc[tp][tc][j] = 0.f;
-      for (const int end = s + nds; s < end; ++s) stage(s, S, acc, f0, f1);
-      epi(acc, g, reinterpret_cast<const float*>(at(s - 1) + Z::AB + Z::BBY));
+      for (const int end = s + nds; s < end; ++s) stage(s, S, s < landed, acc, f0, f1);
+      epi(acc, g, at(s - 1));
+      if (STORES) landed = s + 2;
     }
   }
 };
@@ -281,6 +289,9 @@ __device__ __forceinline__ bool raster_place(const Raster& r, int id, int& a, in
   return sup < r.supers && a < r.na && b < r.nb;
 }
 
+// (by value: a conditional between array elements puts the array into memory)
+__device__ __forceinline__ float pick(bool c, float a, float b) { return c ? a : b; }
+
 // One workgroup: 256 rows of X by a share of the column blocks (all shares within one
 // block of a size).
 struct ScoreArgs {
@@ -292,10 +303,13 @@ struct ScoreArgs {
   int64_t ld;            // bytes of a row
   int V, chunks;         // 16-byte chunks of a row
   float scale;
-  Raster grid;           // shares by row blocks
-  float4* part;          // [B, splits, rows]
+  int vb0, nvb;          // the column blocks of this launch
+  Raster grid;           // shares of them by row blocks
+  int share0, shares;    // the first one's place among all of a row's
+  float4* part;          // [B, shares, rows]
   float* zt;             // [B, rows]
   float *z, *gmax;       // [B, rows, ldz], [B, rows, groups]
+  const float* bound;    // [B, rows] groups whose best does not exceed it are not stored; NULL: all are
   int64_t ldz, groups;
 };
 
@@ -307,8 +321,8 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   int64_t b;
   if (!raster_place(a.grid, blockIdx.x, sp, mb, b)) return;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int64_t nvb = (a.V + 255) / 256;
-  const int blk0 = (int)(nvb * sp / a.grid.na), blk1 = (int)(nvb * (sp + 1) / a.grid.na);
+  const int blk0 = a.vb0 + (int)((int64_t)a.nvb * sp / a.grid.na);
+  const int blk1 = a.vb0 + (int)((int64_t)a.nvb * (sp + 1) / a.grid.na);
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
@@ -324,18 +338,21 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   NtLoop<DT, 2, BIAS> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
-  Stat st[4];
-  float zt[4];
-  int tgt[4];
-#pragma unroll
-  for (int tp = 0; tp < 4; ++tp) {
-    const int r = in.b0 + wp * 128 + tp * 32 + n;
-    st[tp] = stat_none();
-    zt[tp] = 0.f;
-    tgt[tp] = a.target && r < a.rows ? a.target[b * a.ts + r] : -1;
+  // per row: the target, its score, the bound (in LDS: registers are short)
+  __shared__ int tgt_s[LP_BB];
+  __shared__ float zt_s[LP_BB], bound_s[TOPK ? LP_BB : 1];
+  for (int r = threadIdx.x; r < LP_BB; r += NT_T) {
+    const int64_t row = in.b0 + r;
+    tgt_s[r] = a.target && row < a.rows ? a.target[b * a.ts + row] : -1;
+    if (TOPK) bound_s[r] = a.bound && row < a.rows ? a.bound[b * a.rows + row] : NEG_INF;
   }
+  Stat st[4];
+#pragma unroll
+  for (int tp = 0; tp < 4; ++tp) st[tp] = stat_none();
+  __syncthreads();
   const float c2 = a.scale * LOG2E;
-  auto epi = [&](f32x16(&acc)[4][2], int g, const float* bias) {
+  auto epi = [&](f32x16(&acc)[4][2], int g, char* scratch) {
+    const float* bias = reinterpret_cast<const float*>(scratch + Z::AB + Z::BBY);
     const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
     const bool edge = v0 + 64 > a.V;
     if (BIAS || edge) {  // the scores themselves, with the offsets, into acc
@@ -355,6 +372,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
               const float z = __builtin_fmaf(acc[tp][tc][4 * q + r], a.scale, x[r]);
               acc[tp][tc][4 * q + r] = off ? NEG_INF : z;
             }
+            __builtin_amdgcn_sched_barrier(0);  // one mask at a time: 32 of them spill
           }
         }
     }
@@ -399,56 +417,75 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
       st[tp].s += es;
       st[tp].t += et;
       // the target, if it is among this lane's 32 columns
-      const int rel = tgt[tp] - v0;
+      const int rl = wp * 128 + tp * 32 + n, rel = tgt_s[rl] - v0;
       const bool hit = (unsigned)rel < 64u && ((rel >> 2) & 1) == h;
-      if (__ballot(hit)) {
+      if (__ballot(hit)) {  // halves of its 32 scores by the bits of its place among them
+        float x[16];
 #pragma unroll
-        for (int tc = 0; tc < 2; ++tc)
+        for (int j = 0; j < 16; ++j) x[j] = pick(rel & 32, acc[tp][1][j], acc[tp][0][j]);
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (hit && rel == tc * 32 + 8 * (j >> 2) + 4 * h + (j & 3)) zt[tp] = acc[tp][tc][j] * zs;
+        for (int j = 0; j < 8; ++j) x[j] = pick(rel & 16, x[j + 8], x[j]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = pick(rel & 8, x[j + 4], x[j]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) x[j] = pick(rel & 2, x[j + 2], x[j]);
+        if (hit) zt_s[rl] = pick(rel & 1, x[1], x[0]) * zs;
       }
       if constexpr (TOPK) {
-        const int64_t row = in.b0 + wp * 128 + tp * 32 + n;
+        const int64_t row = in.b0 + rl;
         const float gm = __builtin_fmaxf(lm, __shfl_xor(lm, 32));
-        if (row < a.rows) {
-          if (h == 0 && v0 < a.V) a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = gm;
-          float* zr = a.z + (b * a.rows + row) * a.ldz + v0 + 4 * h;
+        const bool keep = !a.bound || gm > bound_s[rl];
+        if (tp == 0) __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): see run()
+        if (row < a.rows && h == 0 && v0 < a.V)
+          a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = keep ? gm : NEG_INF;
+        // 32 x 32 scores at a time through the wave's eighth of the finished stage's
+        // buffer (row n's 16-byte unit c at c ^ (n & 7)), so that whole lines are written:
+        // straight from the lanes, 32 bytes of each of 32 rows, they took 2.5 times as long
+        const uint64_t kept = __ballot(row < a.rows && keep);
+        if (kept) {
+          float* zr = a.z + (b * a.rows + in.b0 + wp * 128 + tp * 32) * a.ldz + v0;
+          char* sq = scratch + loop.wave * 4096;
 #pragma unroll
-          for (int tc = 0; tc < 2; ++tc)
+          for (int tc = 0; tc < 2; ++tc) {
+            const f32x16& x = acc[tp][tc];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const f32x16& x = acc[tp][tc];
-              *reinterpret_cast<f32x4*>(zr + tc * 32 + 8 * q) =
+            for (int q = 0; q < 4; ++q)
+              nt_at<f32x4>(sq, n * 128 + (((2 * q + h) ^ (n & 7)) << 4)) =
                   f32x4{x[4 * q] * zs, x[4 * q + 1] * zs, x[4 * q + 2] * zs, x[4 * q + 3] * zs};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int r = 8 * i + (lane >> 3), c = lane & 7;
+              const f32x4 y = nt_at<f32x4>(sq, r * 128 + ((c ^ (r & 7)) << 4));
+              if (kept >> r & 1) *reinterpret_cast<f32x4*>(zr + r * a.ldz + tc * 32 + 4 * c) = y;
             }
+          }
         }
       }
     }
   };
-  loop.run(epi);
+  loop.template run<TOPK>(epi);
 
   // the two lanes of a row, then the four waves that share it, in a fixed order
   __syncthreads();
   Stat* sh = reinterpret_cast<Stat*>(smem);  // [4][256]
 #pragma unroll
   for (int tp = 0; tp < 4; ++tp) {
-    const int rl = wp * 128 + tp * 32 + n, rel = tgt[tp] - in.a0;
-    // the score of a target among this share's columns, from the lane that held it
-    if ((unsigned)tgt[tp] < (unsigned)a.V && (unsigned)rel < (unsigned)(in.nblk * 256) &&
-        ((rel >> 2) & 1) == h && ((rel >> 6) & 3) == wc)
-      a.zt[b * a.rows + in.b0 + rl] = zt[tp];
+    const int rl = wp * 128 + tp * 32 + n;
     Stat o = {__shfl_xor(st[tp].m, 32), __shfl_xor(st[tp].s, 32), __shfl_xor(st[tp].t, 32)};
     o = stat_merge(h ? o : st[tp], h ? st[tp] : o);
     if (h == 0) sh[wc * LP_BB + rl] = o;
   }
   __syncthreads();
   for (int r = threadIdx.x; r < LP_BB; r += NT_T) {
+    // a target among this share's columns has its score
+    const int rel = tgt_s[r] - in.a0;
+    if ((unsigned)tgt_s[r] < (unsigned)a.V && (unsigned)rel < (unsigned)(in.nblk * 256))
+      a.zt[b * a.rows + in.b0 + r] = zt_s[r];
     Stat o = sh[r];
 #pragma unroll
     for (int q = 1; q < 4; ++q) o = stat_merge(o, sh[q * LP_BB + r]);
     if (in.b0 + r < a.rows)
-      a.part[(b * a.grid.na + sp) * a.rows + in.b0 + r] = make_float4(o.m, o.s, o.t, 0.f);
+      a.part[(b * a.shares + a.share0 + sp) * a.rows + in.b0 + r] = make_float4(o.m, o.s, o.t, 0.f);
   }
 }
 
@@ -586,6 +623,38 @@ __device__ __forceinline__ float key_score(uint32_t u) {
   return __uint_as_float((u & 0x80000000u) ? (u & 0x7fffffffu) : ~u);
 }
 
+// The k-th largest of a wave's 256 keys, or something below it that exactly k reach.
+__device__ __forceinline__ uint32_t wave_kth(const uint32_t (&x)[4], int k) {
+  uint32_t kth = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t c = kth | (1u << bit);
+    int cnt = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cnt += __popcll(__ballot(x[i] >= c));
+    if (cnt >= k) kth = c;
+    if (cnt == k) break;
+  }
+  return kth;
+}
+
+// A bound for the columns still to come, one wave per row: at least k of the first
+// `groups` groups' bests reach it, so a later group is among a row's k best only if its
+// own best exceeds it (at an equal score the earlier column is the better).
+__global__ __launch_bounds__(256) void bound_kernel(const float* __restrict__ gmax, int64_t rows,
+                                                    int64_t stride, int groups, int k,
+                                                    float* __restrict__ bound) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  uint32_t x[4] = {0, 0, 0, 0};
+  for (int i = lane; i < groups; i += 256)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (i + 64 * j < groups) x[j] = max(x[j], score_key(gmax[row * stride + i + 64 * j]));
+  const uint32_t kth = wave_kth(x, k);
+  if (lane == 0) bound[row] = key_score(kth);
+}
+
 struct FinishArgs {
   const float4* part;
   const float* zt;
@@ -666,8 +735,10 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
     int32_t* ti = a.top_idx + (b * a.ts + row) * k;
     float* tl = a.top_logprob + (b * a.ts + row) * k;
     const bool none = st.s == 0.f;
+    // a group with this best holds nothing (and its scores may not be stored)
+    const uint32_t nothing = score_key(NEG_INF);
     auto put = [&](int j, uint32_t key, int v) {  // forbidden tokens are no alternatives
-      const bool have = key > score_key(NEG_INF) && v < a.V && !none;
+      const bool have = key > nothing && v < a.V && !none;
       ti[j] = have ? v : -1;
       tl[j] = have ? (key_score(key) - st.m) - logs : NEG_INF;
     };
@@ -682,17 +753,10 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
     if (tid == 0) ngroups = nentries = 0;
     __syncthreads();
     if (w == 0) {  // the k-th largest of the thread bests
-      uint32_t x[4], kth = 0;
+      uint32_t x[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = best[lane + 64 * i];
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t c = kth | (1u << bit);
-        int cnt = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) cnt += __popcll(__ballot(x[i] >= c));
-        if (cnt >= k) kth = c;
-        if (cnt == k) break;  // exactly k reach it: bound enough
-      }
+      const uint32_t kth = wave_kth(x, k);
       if (lane == 0) bound_s = kth;
     }
     __syncthreads();
@@ -708,7 +772,7 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
       for (int v = tid; v < a.V; v += 256) entry(v);
     } else {
       for (int i = tid; i < G; i += 256)
-        if (score_key(gm[i]) >= bound) {
+        if (score_key(gm[i]) >= max(bound, nothing + 1)) {
           const int at = atomicAdd(&ngroups, 1);
           if (at < TOP_GROUPS) sel[at] = i;
         }
@@ -721,8 +785,10 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
       }
     }
     __syncthreads();
-    const int n = nentries;  // at least k
+    const int n = nentries;
     if (n <= TOP_ENTRIES) {
+      if (tid >= n && tid < k) put(tid, 0u, -1);  // fewer than k are allowed
+
       // each entry's rank: whichever way they were gathered, the order is the same
       if (tid < n) {
         const uint32_t key = ekey[tid];
@@ -772,7 +838,8 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
     uint32_t key[TOK_MAX_K];  // entry `lane` of each chosen group; groups in ascending order
 #pragma unroll
     for (int i = 0; i < TOK_MAX_K; ++i)
-      key[i] = i < kg ? score_key(zr[(int64_t)sel[i] * LP_GROUP + lane]) : 0u;
+      key[i] = i < kg && score_key(gm[sel[i]]) > nothing
+                   ? score_key(zr[(int64_t)sel[i] * LP_GROUP + lane]) : 0u;
     for (int j = 0; j < k; ++j) {
       uint32_t top = 0;
       int at = -1;
@@ -939,7 +1006,8 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   auto at = [](int rl, int c) {
     return rl * 512 + ((c ^ (((((rl & 7) ^ ((rl >> 5) & 7))) << 2) | ((rl >> 3) & 3))) << 4);
   };
-  auto epi = [&](f32x16(&acc)[4][2], int, const float* bias) {
+  auto epi = [&](f32x16(&acc)[4][2], int, char* scratch) {
+    const float* bias = reinterpret_cast<const float*>(scratch + Z::AB + Z::BBY);
     float bz[2][16];
     if constexpr (BIAS) {
 #pragma unroll
@@ -987,7 +1055,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     }
     __syncthreads();
   };
-  loop.run(epi);
+  loop.template run<false>(epi);
 
   const int64_t vb = in.a0 - a.v0;  // within the block of table rows
   uint16_t* dz = a.dz + b * a.M * a.lv;
@@ -1069,7 +1137,7 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   NtLoop<DT, TCW, false> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
-  auto epi = [&](f32x16(&acc)[4][TCW], int, const float*) {
+  auto epi = [&](f32x16(&acc)[4][TCW], int, char*) {
 #pragma unroll
     for (int tp = 0; tp < 4; ++tp) {
       const int64_t r = in.b0 + wp * 128 + tp * 32 + n;
@@ -1107,7 +1175,7 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
         }
     }
   };
-  loop.run(epi);
+  loop.template run<false>(epi);
 }
 
 // out[b, r, d] = factor * sum over the shares of part[b, s, r, d].
@@ -1134,6 +1202,19 @@ hipError_t launch_few(const FewArgs& q, const LogprobsArgs& a, const LogprobsWs&
   } else {
     if (a.k) few_kernel<DT, CB, false, true><<<grid, 256, 0, s>>>(q);
     else few_kernel<DT, CB, false, false><<<grid, 256, 0, s>>>(q);
+  }
+  return hipGetLastError();
+}
+
+template <int DT>
+hipError_t launch_score(const ScoreArgs& q, const LogprobsArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)q.grid.blocks());
+  if (a.bias) {
+    if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
+    else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
+  } else {
+    if (a.k) score_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(q);
+    else score_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(q);
   }
   return hipGetLastError();
 }
@@ -1170,22 +1251,30 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
       q.V = (int)a.V;
       q.chunks = (int)(w.Dk / 8);
       q.scale = a.scale;
-      q.grid = make_raster(w.plan.splits, (rows + LP_BB - 1) / LP_BB, a.B);
+      q.shares = w.plan.head_splits + w.plan.splits;
       q.part = w.part;
       q.zt = w.zt;
       q.z = w.z;
       q.gmax = w.gmax;
       q.ldz = w.ldz;
       q.groups = w.groups;
-      const dim3 grid((unsigned)q.grid.blocks());
-      if (a.bias) {
-        if (a.k) score_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(q);
-        else score_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(q);
-      } else {
-        if (a.k) score_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(q);
-        else score_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(q);
+      q.bound = nullptr;
+      const int64_t nmb = (rows + LP_BB - 1) / LP_BB;
+      q.vb0 = q.share0 = 0;
+      if (w.plan.head) {
+        q.nvb = w.plan.head;
+        q.grid = make_raster(w.plan.head_splits, nmb, a.B);
+        if ((e = launch_score<DT>(q, a, s)) != hipSuccess) return e;
+        bound_kernel<<<dim3((unsigned)((a.B * rows + 3) / 4)), 256, 0, s>>>(
+            w.gmax, a.B * rows, w.groups, w.plan.head * 4, a.k, w.bound);
+        if ((e = hipGetLastError()) != hipSuccess) return e;
+        q.bound = w.bound;
+        q.vb0 = w.plan.head;
+        q.share0 = w.plan.head_splits;
       }
-      e = hipGetLastError();
+      q.nvb = (int)(w.ldz / 256) - q.vb0;
+      q.grid = make_raster(w.plan.splits, nmb, a.B);
+      e = launch_score<DT>(q, a, s);
     }
     if (e != hipSuccess) return e;
     FinishArgs f;
@@ -1198,7 +1287,7 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
     f.ts = a.M;
     f.ldz = w.ldz;
     f.groups = w.groups;
-    f.splits = w.plan.splits;
+    f.splits = w.plan.head_splits + w.plan.splits;
     f.V = (int)a.V;
     f.k = a.k;
     f.logprob = a.logprob + m0;

@@ -47,6 +47,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // At most this many workgroups come of sharing out column blocks or a contraction:
 // two rounds on 256 CUs (contractions) or four (columns).
 constexpr int64_t SCORE_WGS = 1024, OUT_WGS = 512;
+constexpr int64_t HEAD_SCORES = 1 << 24;  // scores from which alternatives take a head
 
 // Shares of the column blocks: the number with the least rounds of 256 workgroups
 // times what one takes, its blocks and about six stages of filling and emptying.
@@ -72,15 +73,25 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
   if (k) w.plan.rows = std::min(M, std::max<int64_t>(LP_SCORE_BYTES / (B * w.ldz * 4) / 256, 1) * 256);
   const int64_t nmb = cdiv(w.plan.rows, LP_BB), wgs = nmb * B;
   w.plan.few = M <= LP_FEW_M;
-  w.plan.splits = w.plan.few ? (int)cdiv(V, 64) : score_splits(nmb, B, w.ldz / 256, cdiv(w.Dk, LP_DC));
+  const int64_t nvb = w.ldz / 256, stages = cdiv(w.Dk, LP_DC);
+  // A head of an eighth of the columns (of 8 groups for each of the k best at the least)
+  // where storing every score would cost more than two launches: 4,096 x 65,536 x
+  // 1,024, k = 20: 1,014 -> HEAD_US us.
+  if (k && !w.plan.few && B * w.plan.rows * w.ldz >= HEAD_SCORES) {
+    const int64_t head = std::max(nvb / 8, cdiv(8 * k, 4));
+    if (head <= nvb / 4) w.plan.head = (int)head;
+  }
+  if (w.plan.head) w.plan.head_splits = score_splits(nmb, B, w.plan.head, stages);
+  w.plan.splits = w.plan.few ? (int)cdiv(V, 64) : score_splits(nmb, B, nvb - w.plan.head, stages);
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   // B x splits x rows, for any number of shares that these or fewer rows would get
-  take(w.part, (size_t)std::max(std::max(SCORE_WGS, wgs) * LP_BB,
+  take(w.part, (size_t)std::max(2 * std::max(SCORE_WGS, wgs) * LP_BB,
                                 B * std::min(M, LP_FEW_M) * cdiv(V, 64)) * sizeof(float4));
   take(w.zt, (size_t)(B * w.plan.rows) * 4);
   take(w.gmax, k ? (size_t)(B * w.plan.rows * w.groups) * 4 : 0);
   take(w.z, k ? (size_t)(B * w.plan.rows * w.ldz) * 4 : 0);
+  take(w.bound, k ? (size_t)(B * w.plan.rows) * 4 : 0);
   w.total = take.o;
   return w;
 }

@@ -79,7 +79,10 @@ constexpr int64_t LP_FEW_M = 64;
 struct LogprobsPlan {
   int64_t rows;    // rows of a block (all of M for k = 0)
   bool few;        // up to LP_FEW_M rows: a workgroup for every 64 columns and all rows
-  int splits;      // shares of the columns, a workgroup each
+  // k > 0 and many scores: the first `head` column blocks in a launch of their own, whose
+  // scores bound the k best from below; of the others only what exceeds that is stored
+  int head, head_splits;
+  int splits;      // shares of the (other) columns, a workgroup each
 };
 struct LogprobsWs {
   void *xpad, *wpad;  // rows of Dk elements, where D is no multiple of 8
@@ -87,6 +90,7 @@ struct LogprobsWs {
   float* zt;          // [B, rows] score of the target
   float* gmax;        // [B, rows, groups] best score of each group (k > 0)
   float* z;           // [B, rows, ldz] scores (k > 0)
+  float* bound;       // [B, rows] (k > 0)
   int64_t Dk, ldz, groups;
   LogprobsPlan plan;
   size_t total;
