@@ -866,98 +866,190 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
 }
 
 // ---- gradient ------------------------------------------------------------------
-constexpr float F16_UP = 2048.f;  // dz of fp16 rows is stored this much larger
+// dz and the copies of X and W that the two products read are fp16 for both storage
+// types: 11 significant bits against bf16's 8 make dz's rounding an eighth, below that
+// of the results (bf16 dz: dX and dW off by 2.4e-3 of their norm, 1.7e-3 being their own
+// rounding; fp16: 1.7e-3).  Powers of two keep all three in range: each row's dz is
+// stored over gs, at or above max(|g|, |h|), and DZ_UP times larger; X (times gs over
+// the largest gs) and W times what brings their largest value just below 2^14, where
+// fp16 holds every bf16 or fp16 value down to 2^-28 of that exactly.
+constexpr float DZ_UP = 2048.f;
+constexpr int STATS_WGS = 256;  // workgroups of an instance's statistics
 
-// What each position's gradient needs.  fp16: dz is stored over the power of two gs at
-// or above max(|g|, |h|), so that small probabilities stay in range.
+// What each position's gradient needs, and the largest gs and magnitudes: X's of the
+// rows that take part, W's of the tokens that do.  One wave per row.
 template <int DT>
-__global__ __launch_bounds__(256) void grad_rows_kernel(
-    const int32_t* __restrict__ target, const float* __restrict__ lse,
-    const float* __restrict__ ent, const float* __restrict__ g, const float* __restrict__ h,
-    const float* __restrict__ bias, int64_t rows, int64_t M, int V, RowGrad* __restrict__ out) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows; i += (int64_t)gridDim.x * 256) {
+__global__ __launch_bounds__(512) void grad_rows_kernel(
+    const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
+    const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
+    const float* __restrict__ h, const float* __restrict__ bias, int64_t M, int V, int D,
+    RowGrad* __restrict__ out, float4* __restrict__ stats) {
+  __shared__ float sh[8][3];
+  const int64_t b = blockIdx.y;
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = gridDim.x * 8;
+  float gsmax = 0.f;
+  uint32_t mx = 0, mw = 0;  // magnitudes' bits, which order as the values do
+  constexpr uint32_t FIN = DT == DT_BF16 ? 0x7f7f : 0x7bff;  // the largest finite one
+  auto row_max = [&](const uint16_t* p, uint32_t m) {
+    auto one = [&](uint32_t v) {
+      v &= 0x7fffu;
+      return v > FIN ? 0u : v;
+    };
+    if (D % 8 == 0) {
+      for (int d = lane * 8; d < D; d += 512) {
+        const uint4 q = *reinterpret_cast<const uint4*>(p + d);
+        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, max(one(x[e]), one(x[e] >> 16)));
+      }
+    } else {
+      for (int d = lane; d < D; d += 64) m = max(m, one(p[d]));
+    }
+    return m;
+  };
+  for (int64_t m = blockIdx.x * 8 + w; m < M; m += nw) {
+    const int64_t i = b * M + m;
     RowGrad r;
     const int t = target[i];
-    r.target = (unsigned)t < (unsigned)V && (!bias || bias[(i / M) * V + t] != NEG_INF) ? t : -1;
+    r.target = (unsigned)t < (unsigned)V && (!bias || bias[b * V + t] != NEG_INF) ? t : -1;
     r.lse = lse[i];
-    const bool any = r.lse != NEG_INF;
     r.g = r.target >= 0 ? g[i] : 0.f;
     r.h = h ? h[i] : 0.f;
     r.ent = h ? ent[i] : 0.f;
-    r.active = any && (r.g != 0.f || r.h != 0.f);
+    r.active = r.lse != NEG_INF && (r.g != 0.f || r.h != 0.f);
     r.gs = 1.f;
-    if constexpr (DT == DT_F16) {
-      const float m = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
-      int e = 0;
-      if (r.active && m <= __FLT_MAX__) {
-        (void)frexpf(m, &e);
-        e = min(max(e, -120), 120);
-        r.gs = ldexpf(1.f, e);
-        r.g *= ldexpf(1.f, -e);
-        r.h *= ldexpf(1.f, -e);
-      }
-    }
     r.pad = 0;
-    out[i] = r;
+    const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
+    if (r.active && big <= __FLT_MAX__) {
+      int e;
+      (void)frexpf(big, &e);
+      e = min(max(e, -120), 120);
+      r.gs = ldexpf(1.f, e);
+      r.g *= ldexpf(1.f, -e);
+      r.h *= ldexpf(1.f, -e);
+    }
+    if (lane == 0) out[i] = r;
+    if (r.active) {
+      gsmax = __builtin_fmaxf(gsmax, r.gs);
+      mx = row_max(X + i * D, mx);
+    }
   }
-}
-
-// The largest gs of an instance's active rows.
-__global__ __launch_bounds__(1024) void grad_gsmax_kernel(const RowGrad* __restrict__ rows,
-                                                          int64_t M, float* __restrict__ gsmax) {
-  __shared__ float s[16];
-  const int64_t b = blockIdx.x;
-  float m = 0.f;
-  for (int64_t i = threadIdx.x; i < M; i += 1024)
-    if (rows[b * M + i].active) m = __builtin_fmaxf(m, rows[b * M + i].gs);
+  for (int v = blockIdx.x * 8 + w; v < V; v += nw)
+    if (!bias || bias[b * V + v] != NEG_INF) mw = row_max(W + (b * V + v) * D, mw);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) m = __builtin_fmaxf(m, __shfl_xor(m, d));
-  if ((threadIdx.x & 63) == 0) s[threadIdx.x >> 6] = m;
+  for (int d = 1; d < 64; d <<= 1) {
+    mx = max(mx, (uint32_t)__shfl_xor((int)mx, d));
+    mw = max(mw, (uint32_t)__shfl_xor((int)mw, d));
+  }
+  if (lane == 0) {
+    sh[w][0] = gsmax;
+    sh[w][1] = Elem<DT>::widen((uint16_t)mx);
+    sh[w][2] = Elem<DT>::widen((uint16_t)mw);
+  }
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < 16; ++i) m = __builtin_fmaxf(m, s[i]);
-    gsmax[b] = m > 0.f ? m : 1.f;
+    float4 o = make_float4(0, 0, 0, 0);
+    for (int i = 0; i < 8; ++i) {
+      o.x = __builtin_fmaxf(o.x, sh[i][0]);
+      o.y = __builtin_fmaxf(o.y, sh[i][1]);
+      o.z = __builtin_fmaxf(o.z, sh[i][2]);
+    }
+    stats[b * gridDim.x + blockIdx.x] = o;
   }
 }
 
-// in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance -> out [nb, C, ldo], zeros up
-// to np.  Rows that take no part become zeros: of X those without a gradient (the others
-// times gs / gsmax for fp16), of W the forbidden tokens.
+// The power of two that brings values of magnitude up to m below 2^14.
+__device__ __forceinline__ float up_to_2_14(float m) {
+  if (!(m > 0.f)) return 1.f;
+  int e;
+  (void)frexpf(m, &e);
+  return ldexpf(1.f, min(14 - e, 126));
+}
+// scales[b] = (largest gs, factor of X, factor of W).
+__global__ __launch_bounds__(64) void grad_scales_kernel(const float4* __restrict__ stats, int n,
+                                                         float4* __restrict__ scales) {
+  const int64_t b = blockIdx.x;
+  float4 o = make_float4(0, 0, 0, 0);
+  for (int i = threadIdx.x; i < n; i += 64) {
+    const float4 s = stats[b * n + i];
+    o.x = __builtin_fmaxf(o.x, s.x);
+    o.y = __builtin_fmaxf(o.y, s.y);
+    o.z = __builtin_fmaxf(o.z, s.z);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    o.x = __builtin_fmaxf(o.x, __shfl_xor(o.x, d));
+    o.y = __builtin_fmaxf(o.y, __shfl_xor(o.y, d));
+    o.z = __builtin_fmaxf(o.z, __shfl_xor(o.z, d));
+  }
+  if (threadIdx.x == 0)
+    scales[b] = make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_14(o.y), up_to_2_14(o.z), 0.f);
+}
+
+// Transposed fp16 copies: in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance, times a
+// factor, -> out [nb, C, ldo], zeros up to np.  Rows that take no part become zeros: of X
+// those without a gradient (the others times gs over the largest too), of W the forbidden
+// tokens.  64 x 64 values at a time: a thread reads 8 columns of two rows and stores them
+// in LDS as pairs of rows, and writes 8 rows of two columns.
+struct CopyJob {
+  const uint16_t* in;
+  int64_t R, r0, nr, np, ldo;
+  const RowGrad* rows;  // of X
+  const float* bias;    // of W
+  uint16_t* out;
+  int tiles;  // np / 64; 0: no such job
+};
 template <int DT>
-__global__ __launch_bounds__(256) void transpose_kernel(
-    const uint16_t* __restrict__ in, int64_t R, int C, int64_t r0, int64_t nr, int64_t np, int64_t ldo,
-    const RowGrad* __restrict__ rows, const float* __restrict__ gsmax,
-    const float* __restrict__ bias, uint16_t* __restrict__ out) {
-  __shared__ uint16_t tile[64][66];
-  const int64_t b = blockIdx.z, rt = (int64_t)blockIdx.x * 64;
+__global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
+                                                   const float4* __restrict__ scales) {
+  constexpr int LD = 33;  // pairs from column to column: no conflicts on writes
+  __shared__ uint32_t tile[64 * LD];
+  const bool is_x = (int)blockIdx.x < x.tiles;
+  const CopyJob j = is_x ? x : w;
+  const int64_t b = blockIdx.z, rt = (int64_t)((int)blockIdx.x - (is_x ? 0 : x.tiles)) * 64;
   const int ct = blockIdx.y * 64, t = threadIdx.x;
-  in += b * R * C;
-  for (int i = t; i < 64 * 64; i += 256) {
-    const int64_t r = rt + i / 64;
-    const int c = ct + i % 64;
-    uint16_t v = 0;
-    if (r < nr && c < C) {
-      bool use = true;
-      float f = 1.f;
-      if (rows) {
-        const RowGrad& g = rows[b * R + r0 + r];
-        use = g.active;
-        if (DT == DT_F16) f = g.gs / gsmax[b];
+  const float4 sc = scales[b];
+#pragma unroll
+  for (int u = 0; u < 1; ++u) {
+    const int c8 = t % 8, rp = t / 8;  // 8 columns of rows 2 rp, 2 rp + 1
+    uint16_t v[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = rt + 2 * rp + i;
+      float f = 0.f;
+      if (r < j.nr) {
+        const int64_t ri = b * j.R + j.r0 + r;
+        if (is_x) f = j.rows[ri].active ? j.rows[ri].gs / sc.x * sc.y : 0.f;
+        else f = j.bias && j.bias[ri] == NEG_INF ? 0.f : sc.z;
       }
-      if (bias) use = bias[b * R + r0 + r] != NEG_INF;
-      if (use) {
-        v = in[(r0 + r) * C + c];
-        if (DT == DT_F16 && rows) v = Elem<DT>::narrow(Elem<DT>::widen(v) * f);
+      alignas(16) uint16_t x8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+      const int c = ct + 8 * c8;
+      if (f != 0.f && c < C) {
+        const uint16_t* p = j.in + (b * j.R + j.r0 + r) * C + c;
+        if (C % 8 == 0) {
+          *reinterpret_cast<uint4*>(x8) = *reinterpret_cast<const uint4*>(p);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c + e < C) x8[e] = p[e];
+        }
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        v[i][e] = f != 0.f ? Elem<DT_F16>::narrow(Elem<DT>::widen(x8[e]) * f) : (uint16_t)0;
     }
-    tile[i / 64][i % 64] = v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      tile[(8 * c8 + e) * LD + rp] = v[0][e] | ((uint32_t)v[1][e] << 16);
   }
   __syncthreads();
-  out += b * C * ldo;
-  for (int i = t; i < 64 * 64; i += 256) {
-    const int c = ct + i / 64;
-    const int64_t r = rt + i % 64;
-    if (c < C && r < np) out[c * ldo + r] = tile[i % 64][i / 64];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int r8 = t % 8, cl = t / 8 + 32 * u, c = ct + cl;
+    const int64_t r = rt + 8 * r8;
+    const uint32_t* q = tile + cl * LD + 4 * r8;
+    if (c < C && r < j.np)
+      *reinterpret_cast<uint4*>(j.out + (b * C + c) * j.ldo + r) = make_uint4(q[0], q[1], q[2], q[3]);
   }
 }
 
@@ -975,7 +1067,7 @@ struct DzArgs {
   Raster grid;
 };
 
-// dz of 256 positions by 256 table rows, rounded to 16 bits, and its transpose: the
+// dz of 256 positions by 256 table rows in fp16, and its transpose: the
 // tile goes through LDS so that both are written in whole lines.
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
@@ -1045,8 +1137,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
             const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
             float dz = -p * __builtin_fmaf(rg.h, __builtin_fmaxf(lp, -1e30f) + rg.ent, rg.g);
             if (v == rg.target) dz += rg.g;
-            if (DT == DT_F16) dz *= F16_UP;
-            w[r] = use ? Elem<DT>::narrow(dz) : (uint16_t)0;
+            w[r] = use ? Elem<DT_F16>::narrow(dz * DZ_UP) : (uint16_t)0;
           }
           const int c = wc * 8 + tc * 4 + q;
           nt_at<uint2>(smem, at(rl, c) + 8 * h) =
@@ -1098,18 +1189,51 @@ struct OutArgs {
   int D, chunks, per;  // chunks of the contraction, stages of a share
   int splits, mode;
   float factor;
-  const RowGrad* rows;  // times rows[r].gs, if given
-  const float* gsmax;   // times gsmax[b], if given
+  const RowGrad* rows;   // dX: times gs of the row, over W's factor
+  const float4* scales;  // dW (rows NULL): times the largest gs, over X's factor
   uint16_t* out;
   float* f32;          // part [nb, splits, R, D] or acc [R, D]
   Raster grid;         // instances: the shares of each
 };
 
-__device__ __forceinline__ float out_factor(float f, const RowGrad* rows, const float* gsmax,
-                                            int64_t b, int64_t os, int64_t r) {
-  if (rows) f *= rows[b * os + r].gs;
-  if (gsmax) f *= gsmax[b];
-  return f;
+__device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b, int64_t r) {
+  const float4 s = a.scales[b];
+  return a.rows ? a.factor / s.z * a.rows[b * a.os + r].gs : a.factor / s.y * s.x;
+}
+
+// Eight consecutive results of a row (those below D) from `v`.
+template <int DT>
+__device__ __forceinline__ void out_store(const OutArgs& a, int64_t b, int sp, int64_t r, int d,
+                                          float (&v)[8]) {
+  if (a.mode == OUT_16) {
+    const float f = out_factor(a, b, r);
+    uint16_t* o = a.out + (b * a.os + r) * a.D + d;
+    alignas(16) uint16_t x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = Elem<DT>::narrow(v[e] * f);
+    if (a.D % 8 == 0) {
+      *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(x);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (d + e < a.D) o[e] = x[e];
+    }
+  } else {
+    float* p = a.mode == OUT_PART ? a.f32 + ((b * a.splits + sp) * a.R + r) * a.D + d
+                                  : a.f32 + r * a.D + d;
+    if (a.D % 8 == 0) {
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        f32x4 x = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+        if (a.mode == OUT_ADD) x += *reinterpret_cast<const f32x4*>(p + e);
+        *reinterpret_cast<f32x4*>(p + e) = x;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (d + e < a.D) p[e] = a.mode == OUT_ADD ? p[e] + v[e] : v[e];
+    }
+  }
 }
 
 template <int DT, int TCW>
@@ -1134,61 +1258,69 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   in.c0 = sp * a.per * 4;
   in.c1 = min(a.chunks, in.c0 + a.per * 4);
   in.nblk = 1;
-  NtLoop<DT, TCW, false> loop;
+  NtLoop<DT_F16, TCW, false> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   auto epi = [&](f32x16(&acc)[4][TCW], int, char*) {
+    // 32 rows by 32 TCW columns at a time through the wave's own LDS, so that lines are
+    // written whole: row n's 16-byte unit c at c ^ (n & 7)
+    __syncthreads();  // every wave has read its last stage
+    char* sq = smem + loop.wave * (4096 * TCW);
+    constexpr int LPR = 4 * TCW, RPI = 64 / LPR;  // lanes a row, rows a step
+    const int d = in.a0 + wc * 32 * TCW + 8 * (lane % LPR);
 #pragma unroll
     for (int tp = 0; tp < 4; ++tp) {
-      const int64_t r = in.b0 + wp * 128 + tp * 32 + n;
-      if (r >= a.R) continue;
-      const float f = a.mode == OUT_16 ? out_factor(a.factor, a.rows, a.gsmax, b, a.os, r) : 1.f;
-      uint16_t* o = a.out + (b * a.os + r) * a.D;
-      float* p = a.mode == OUT_PART ? a.f32 + ((b * a.splits + sp) * a.R + r) * a.D : a.f32 + r * a.D;
 #pragma unroll
       for (int tc = 0; tc < TCW; ++tc)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const int d = in.a0 + (wc * TCW + tc) * 32 + 8 * q + 4 * h;
-          if (a.mode == OUT_16) {
-            uint16_t w[4];
+        for (int q = 0; q < 4; ++q)
+          nt_at<f32x4>(sq, n * (128 * TCW) + (((8 * tc + 2 * q + h) ^ (n & 7)) << 4)) =
+              f32x4{acc[tp][tc][4 * q], acc[tp][tc][4 * q + 1], acc[tp][tc][4 * q + 2],
+                    acc[tp][tc][4 * q + 3]};
+#pragma unroll 1
+      for (int i = 0; i < 32; i += RPI) {
+        const int rl = i + lane / LPR;
+        const int64_t r = in.b0 + wp * 128 + tp * 32 + rl;
+        float v[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) w[e] = Elem<DT>::narrow(acc[tp][tc][4 * q + e] * f);
-            if (a.D % 4 == 0) {
-              if (d < a.D)
-                *reinterpret_cast<uint2*>(o + d) =
-                    make_uint2(w[0] | ((uint32_t)w[1] << 16), w[2] | ((uint32_t)w[3] << 16));
-            } else {
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (d + e < a.D) o[d + e] = w[e];
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (d + e < a.D) {
-                float v = acc[tp][tc][4 * q + e];
-                if (a.mode == OUT_ADD) v += p[d + e];
-                p[d + e] = v;
-              }
-          }
-        }
+        for (int e = 0; e < 2; ++e)
+          *reinterpret_cast<f32x4*>(v + 4 * e) =
+              nt_at<f32x4>(sq, rl * (128 * TCW) + (((2 * (lane % LPR) + e) ^ (rl & 7)) << 4));
+        if (r < a.R && d < a.D) out_store<DT>(a, b, sp, r, d, v);
+      }
     }
   };
   loop.template run<false>(epi);
 }
 
-// out[b, r, d] = factor * sum over the shares of part[b, s, r, d].
+// out[b, r, d] = the sum over the shares of part[b, s, r, d] in their order, times its
+// factor; eight results a thread.
 template <int DT>
 __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs a, int64_t nb) {
-  const int64_t n = a.R * a.D;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < nb * n; i += (int64_t)gridDim.x * 256) {
-    const int64_t b = i / n, j = i % n, r = j / a.D;
-    const float* p = a.f32 + b * a.splits * n + j;
-    float v = 0.f;
-    for (int s = 0; s < a.splits; ++s) v += p[s * n];
-    a.out[b * a.os * a.D + j] =
-        Elem<DT>::narrow(v * out_factor(a.factor, a.rows, a.gsmax, b, a.os, r));
+  const int dc = (a.D + 7) / 8;
+  const int64_t n = nb * a.R * dc;
+  OutArgs o = a;
+  o.mode = OUT_16;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t br = i / dc, b = br / a.R, r = br % a.R;
+    const int d = (int)(i % dc) * 8;
+    const float* p = a.f32 + (b * a.splits * a.R + r) * a.D + d;
+    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s = 0; s < a.splits; ++s, p += a.R * a.D) {
+      if (a.D % 8 == 0) {
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const f32x4 x = *reinterpret_cast<const f32x4*>(p + e);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[e + k] += x[k];
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (d + e < a.D) v[e] += p[e];
+      }
+    }
+    out_store<DT>(o, b, 0, r, d, v);
   }
 }
 
@@ -1307,6 +1439,13 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
 }
 
 template <int DT>
+hipError_t launch_reduce(const OutArgs& q, int64_t nb, hipStream_t s) {
+  const int64_t n = nb * q.R * ((q.D + 7) / 8);
+  out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, nb);
+  return hipGetLastError();
+}
+
+template <int DT>
 hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
   const bool narrow = q.D <= 128;
   const int ba = narrow ? 128 : 256, nst = (q.chunks + 3) / 4;
@@ -1318,9 +1457,7 @@ hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
   else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(q);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || q.mode != OUT_PART) return e;
-  const int64_t n = nb * q.R * q.D;
-  out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, nb);
-  return hipGetLastError();
+  return launch_reduce<DT>(q, nb, s);
 }
 
 template <int DT>
@@ -1333,29 +1470,28 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     X = (const char*)w.xpad;
     W = (const char*)w.wpad;
   }
-  const int64_t rows = a.B * a.M, lm = grad_ld(w.Mp);
-  grad_rows_kernel<DT><<<dim3((unsigned)std::min<int64_t>((rows + 255) / 256, 1 << 16)), 256, 0, s>>>(
-      a.target, a.lse, a.entropy, a.g, a.h, a.bias, rows, a.M, (int)a.V, w.rows);
+  const int64_t lm = grad_ld(w.Mp);
+  // a wave has four rows of X and W or more, up to a workgroup per CU in all
+  const int64_t wgs = std::max<int64_t>(1, std::min<int64_t>(STATS_WGS, (a.M + a.V) / 32));
+  grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
+      (const uint16_t*)a.X, (const uint16_t*)a.W, a.target, a.lse, a.entropy, a.g, a.h, a.bias, a.M,
+      (int)a.V, (int)a.D, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  constexpr bool f16 = DT == DT_F16;
-  if (f16) {
-    grad_gsmax_kernel<<<dim3((unsigned)a.B), 1024, 0, s>>>(w.rows, a.M, w.gsmax);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
+  grad_scales_kernel<<<dim3((unsigned)a.B), 64, 0, s>>>(w.stats, (int)wgs, w.scales);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);
     const RowGrad* rg = w.rows + b0 * a.M;
-    const float* gsmax = f16 ? w.gsmax + b0 : nullptr;
+    const float4* scales = w.scales + b0;
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
-    transpose_kernel<DT><<<dim3((unsigned)(w.Mp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
-        (const uint16_t*)a.X + b0 * a.M * a.D, a.M, (int)a.D, 0, a.M, w.Mp, lm, rg, gsmax, nullptr,
-        (uint16_t*)w.xt);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
       const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
-      transpose_kernel<DT><<<dim3((unsigned)(vp / 64), (unsigned)((a.D + 63) / 64), (unsigned)nb), 256, 0, s>>>(
-          (const uint16_t*)a.W + b0 * a.V * a.D, a.V, (int)a.D, v0, nv, vp, lv, nullptr, nullptr, bias,
-          (uint16_t*)w.wt);
+      const CopyJob jx{(const uint16_t*)a.X + b0 * a.M * a.D, a.M, 0, a.M, w.Mp, lm, rg, nullptr,
+                       (uint16_t*)w.xt, v0 ? 0 : (int)(w.Mp / 64)};
+      const CopyJob jw{(const uint16_t*)a.W + b0 * a.V * a.D, a.V, v0, nv, vp, lv, nullptr, bias,
+                       (uint16_t*)w.wt, (int)(vp / 64)};
+      copy_kernel<DT><<<dim3((unsigned)(jx.tiles + jw.tiles), (unsigned)((a.D + 63) / 64), (unsigned)nb),
+                        256, 0, s>>>(jx, jw, (int)a.D, scales);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       DzArgs d;
       d.X = X + b0 * a.M * w.Dk * 2;
@@ -1394,8 +1530,9 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.bs = a.M * q.ld;
       q.R = q.os = a.M;
       q.chunks = (int)(vp / 8);
-      q.factor = f16 ? a.scale / F16_UP : a.scale;
-      q.rows = f16 ? rg : nullptr;
+      q.factor = a.scale / DZ_UP;
+      q.rows = rg;
+      q.scales = scales;
       q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
       q.mode = !whole ? (v0 ? OUT_ADD : OUT_FIRST) : w.sx > 1 ? OUT_PART : OUT_16;
       q.f32 = whole ? w.part : w.accx;
@@ -1410,7 +1547,6 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.os = a.V;
       q.chunks = (int)(w.Mp / 8);
       q.rows = nullptr;
-      q.gsmax = gsmax;
       q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
       q.mode = w.sw > 1 ? OUT_PART : OUT_16;
       q.f32 = w.part;
@@ -1421,13 +1557,12 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.D = (int)a.D;
       q.R = q.os = a.M;
       q.splits = 1;
-      q.factor = f16 ? a.scale / F16_UP : a.scale;
-      q.rows = f16 ? rg : nullptr;
+      q.factor = a.scale / DZ_UP;
+      q.rows = rg;
+      q.scales = scales;
       q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
       q.f32 = w.accx;
-      const int64_t n = a.M * a.D;
-      out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, 1);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      if ((e = launch_reduce<DT>(q, 1, s)) != hipSuccess) return e;
     }
   }
   return hipSuccess;

@@ -118,7 +118,8 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   take(w.rows, (size_t)(B * M) * sizeof(RowGrad));
-  take(w.gsmax, (size_t)B * 4);
+  take(w.stats, (size_t)(B * 256) * sizeof(float4));
+  take(w.scales, (size_t)B * sizeof(float4));
   // sizes that never shrink as M grows, whatever the plan then is
   // (and 64 more elements a row: grad_ld)
   const size_t dz = (size_t)(std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2) +

@@ -109,15 +109,15 @@ struct LogprobsArgs {
 };
 
 // tokens_logprobs_grad.  dz of a block of table rows (Vc of them; all, where it
-// fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in 16
-// bits, and both products read it and transposed copies of X and W.
+// fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in fp16,
+// and both products read it and transposed fp16 copies of X and W.
 constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
 struct RowGrad {  // one position
   float g, h;     // gradients of the log probability and the entropy, over `gs`
   float lse, ent;
   int target;     // -1: none
   int active;     // takes part at all
-  float gs;       // a power of two: what dz of this row is divided by (fp16; else 1)
+  float gs;       // a power of two: what g, h and so dz of this row are divided by
   int pad;
 };
 // Elements from row to row of dz and the copies: 128 bytes past a multiple of 1 KiB, so
@@ -126,7 +126,8 @@ inline int64_t grad_ld(int64_t n) { return n % 512 == 0 ? n + 64 : n; }
 struct GradWs {
   void *xpad, *wpad;
   RowGrad* rows;    // [B, M]
-  float* gsmax;     // [B] largest gs
+  float4* stats;    // [B, workgroups] largest gs and magnitudes of X and W
+  float4* scales;   // [B] the largest gs, the factors of X and W
   void *dz, *dzt;   // [nb, M, grad_ld(Vp)], [nb, Vp, grad_ld(Mp)]
   void *xt, *wt;    // [nb, D, grad_ld(Mp)], [nb, D, grad_ld(Vp)]
   float* accx;      // [M, D] dX over the blocks of table rows, where there are several
