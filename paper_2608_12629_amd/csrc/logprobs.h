@@ -35,6 +35,13 @@ __device__ const uint4 nt_zero = {0, 0, 0, 0};
 __device__ __forceinline__ uint32_t nt_lds(char* lds) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(lds);
 }
+// A pointer that all lanes share, in scalar registers.
+__device__ __forceinline__ const char* nt_uniform(const char* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((int)(uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((int)(uint32_t)(v >> 32));
+  return (const char*)(((uint64_t)hi << 32) | lo);
+}
 __device__ __forceinline__ void nt_dma16(const char* base, uint32_t off, char* lds) {
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1"
                :
@@ -109,7 +116,7 @@ struct NtLoop {
 
   __device__ __forceinline__ void block_rows(int blk) {
     const int a0 = in.a0 + blk * Z::BA, last = in.nA - 1 - a0, r = tid >> 2;
-    ab = in.A + (int64_t)a0 * in.lda + in.c0 * 16;
+    ab = nt_uniform(in.A + (int64_t)a0 * in.lda + in.c0 * 16);
 #pragma unroll
     for (int u = 0; u < TCW; ++u)
       ao[u] = (uint32_t)max(min(r + 128 * u, last), 0) * (uint32_t)in.lda + cc * 16;
@@ -125,7 +132,7 @@ struct NtLoop {
     cc = (tid & 3) ^ nt_swz(tid >> 2);
     nds = (in.c1 - in.c0 + 3) / 4;
     iblk = id = 0;
-    bb = in.B + (int64_t)in.b0 * in.ldb + in.c0 * 16;
+    bb = nt_uniform(in.B + (int64_t)in.b0 * in.ldb + in.c0 * 16);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
       bo[u] = (uint32_t)min((tid >> 2) + 128 * u, in.nB - 1 - in.b0) * (uint32_t)in.ldb + cc * 16;
@@ -277,20 +284,32 @@ __device__ __forceinline__ Stat stat_merge(Stat a, Stat b) {
 }
 
 // ---- scores --------------------------------------------------------------------
+// Share `sp` of n blocks among k: the first block past it, in a scalar register (the
+// division runs on the vector ALU, whose results the compiler takes for different).
+__device__ __forceinline__ int share_end(int n, int sp, int k) {
+  return __builtin_amdgcn_readfirstlane((int)((int64_t)n * sp / k));
+}
+
 // Workgroup `id`: its blocks of A and B and instance; false past the last one.
 __device__ __forceinline__ bool raster_place(const Raster& r, int id, int& a, int& b, int64_t& inst) {
   const int xcd = id & 7, j = id >> 3, size = r.ga * r.gb;
   const int64_t sup = (int64_t)(j / size) * 8 + xcd;
   const int nsa = (r.na + r.ga - 1) / r.ga, nsb = (r.nb + r.gb - 1) / r.gb, in = j % size;
-  inst = sup / (nsa * nsb);
-  const int at = (int)(sup % (nsa * nsb));
-  a = at / nsb * r.ga + in / r.gb;
-  b = at % nsb * r.gb + in % r.gb;
+  const int i = __builtin_amdgcn_readfirstlane((int)(sup / (nsa * nsb)));
+  const int at = (int)(sup - (int64_t)i * (nsa * nsb));
+  inst = i;
+  a = __builtin_amdgcn_readfirstlane(at / nsb * r.ga + in / r.gb);
+  b = __builtin_amdgcn_readfirstlane(at % nsb * r.gb + in % r.gb);
   return sup < r.supers && a < r.na && b < r.nb;
 }
 
 // (by value: a conditional between array elements puts the array into memory)
 __device__ __forceinline__ float pick(bool c, float a, float b) { return c ? a : b; }
+
+__device__ __forceinline__ uint32_t half2_bits(float a, float b) {
+  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});  // to nearest even
+}
 
 // One workgroup: 256 rows of X by a share of the column blocks (all shares within one
 // block of a size).
@@ -321,8 +340,8 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   int64_t b;
   if (!raster_place(a.grid, blockIdx.x, sp, mb, b)) return;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
-  const int blk0 = a.vb0 + (int)((int64_t)a.nvb * sp / a.grid.na);
-  const int blk1 = a.vb0 + (int)((int64_t)a.nvb * (sp + 1) / a.grid.na);
+  const int blk0 = a.vb0 + share_end(a.nvb, sp, a.grid.na);
+  const int blk1 = a.vb0 + share_end(a.nvb, sp + 1, a.grid.na);
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
@@ -1064,20 +1083,25 @@ struct DzArgs {
   float scale;
   uint16_t *dz, *dzt;  // [nb, M, lv], [nb, Vp, lm], zeros up to Vp and Mp
   int64_t Vp, Mp, lv, lm;
-  Raster grid;
+  Raster grid;         // shares of the block's 256-column blocks by row blocks
 };
 
-// dz of 256 positions by 256 table rows in fp16, and its transpose: the
-// tile goes through LDS so that both are written in whole lines.
-template <int DT, bool BIAS>
+// dz of 256 positions by a share of the column blocks, in fp16, and its transpose.  The
+// scores come as in score_kernel; with the row's constants c0 = -(h entropy + g) and c1 =
+// -h ln 2 (times DZ_UP), dz = 2^l (c0 + c1 l), l = log2 p one fma of the accumulator, and g
+// more at the target.  32 x 64 values at a time go through the wave's eighth of the
+// finished stage's buffer, so that lines of both results are written whole.
+template <int DT, bool BIAS, bool ENT>
 __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   using Z = NtSize<2, BIAS>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
-  static_assert(Z::SMEM >= 256 * 512, "the tile fits the stages");
-  int ab, bb;
+  __shared__ float4 row_s[LP_BB];  // c0, c1, lse in units of log 2, g
+  __shared__ int tgt_s[LP_BB];     // -1: none; -2: the row takes no part
+  int sp, bb;
   int64_t b;
-  if (!raster_place(a.grid, blockIdx.x, ab, bb, b)) return;
-  const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
+  if (!raster_place(a.grid, blockIdx.x, sp, bb, b)) return;
+  const int nvb = (a.nv + 255) / 256;
+  const int blk0 = share_end(nvb, sp, a.grid.na), blk1 = share_end(nvb, sp + 1, a.grid.na);
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
@@ -1085,95 +1109,115 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   in.lda = in.ldb = a.ld;
   in.nA = a.v0 + a.nv;
   in.nB = (int)a.M;
-  in.a0 = a.v0 + ab * 256;
+  in.a0 = a.v0 + blk0 * 256;
   in.b0 = bb * LP_BB;
   in.c0 = 0;
   in.c1 = a.chunks;
-  in.nblk = 1;
+  in.nblk = blk1 - blk0;
+  for (int r = threadIdx.x; r < LP_BB; r += NT_T) {
+    RowGrad rg;
+    rg.active = 0;
+    if (in.b0 + r < a.M) rg = a.rows[b * a.M + in.b0 + r];
+    row_s[r] = make_float4(-DZ_UP * __builtin_fmaf(rg.h, rg.ent, rg.g), -DZ_UP * LN2 * rg.h,
+                           rg.lse * LOG2E, DZ_UP * rg.g);
+    tgt_s[r] = rg.active ? rg.target : -2;
+  }
+  __syncthreads();
   NtLoop<DT, 2, BIAS> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
-  // row rl of the tile: 16-byte chunk c at c ^ f(rl), so that lanes 1 or 8 rows apart
-  // meet different banks
-  auto at = [](int rl, int c) {
-    return rl * 512 + ((c ^ (((((rl & 7) ^ ((rl >> 5) & 7))) << 2) | ((rl >> 3) & 3))) << 4);
-  };
-  auto epi = [&](f32x16(&acc)[4][2], int, char* scratch) {
+  const float c2 = a.scale * LOG2E;
+  uint16_t* dz = a.dz + b * a.M * a.lv;
+  uint16_t* dzt = a.dzt + b * a.Vp * a.lm;
+  auto epi = [&](f32x16(&acc)[4][2], int g, char* scratch) {
+    // the lane as a new value, or the addresses below stay in registers through the loop
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int n = lane & 31, h = lane >> 5;
     const float* bias = reinterpret_cast<const float*>(scratch + Z::AB + Z::BBY);
-    float bz[2][16];
-    if constexpr (BIAS) {
-#pragma unroll
-      for (int tc = 0; tc < 2; ++tc)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) bz[tc][4 * q + r] = x[r];
-        }
-    }
-    __syncthreads();  // every wave has read its last stage (and its bias)
+    const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
+    const bool edge = v0 + 64 > in.nA;
+    char* sq = scratch + loop.wave * 4096;
+    // unit u (8 bytes: 4 columns) of row r at u ^ (r & 15)
+    auto at = [&](int r, int u) { return r * 128 + ((u ^ (r & 15)) << 3); };
 #pragma unroll
     for (int tp = 0; tp < 4; ++tp) {
       const int rl = wp * 128 + tp * 32 + n;
-      RowGrad rg;
-      rg.active = 0;
-      if (in.b0 + rl < a.M) rg = a.rows[b * a.M + in.b0 + rl];
-      const int v0 = in.a0 + wc * 64 + 4 * h;
+      const float4 rc = row_s[rl];
+      const int tgt = tgt_s[rl], rel = tgt - v0 - 4 * h;
+      const uint32_t keep = tgt == -2 ? 0u : ~0u;
+      const bool hit = (unsigned)(tgt - v0) < 64u && (((tgt - v0) >> 2) & 1) == h;
+      const bool hits = __ballot(hit) != 0;
 #pragma unroll
       for (int tc = 0; tc < 2; ++tc)
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          uint16_t w[4];
+          f32x4 bz = {0, 0, 0, 0};
+          if constexpr (BIAS)
+            bz = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
+          float y[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int j = 4 * q + r, v = v0 + tc * 32 + 8 * q + r;
-            float z = acc[tp][tc][j] * a.scale;
-            bool use = rg.active && v < in.nA;
-            if constexpr (BIAS) {
-              z = __builtin_fmaf(acc[tp][tc][j], a.scale, bz[tc][j]);
-              use = use && bz[tc][j] != NEG_INF;
-            }
-            const float lp = z - rg.lse;
-            const float p = __builtin_amdgcn_exp2f(lp * LOG2E);
-            float dz = -p * __builtin_fmaf(rg.h, __builtin_fmaxf(lp, -1e30f) + rg.ent, rg.g);
-            if (v == rg.target) dz += rg.g;
-            w[r] = use ? Elem<DT_F16>::narrow(dz * DZ_UP) : (uint16_t)0;
+            const float x = acc[tp][tc][4 * q + r];
+            float l;
+            if constexpr (BIAS)  // in natural units: an offset may be the type's lowest value
+              l = __builtin_fmaf(__builtin_fmaf(x, a.scale, bz[r]), LOG2E, -rc.z);
+            else
+              l = __builtin_fmaf(x, c2, -rc.z);
+            const float p = __builtin_amdgcn_exp2f(l);
+            if constexpr (ENT)
+              y[r] = p * __builtin_fmaf(BIAS ? __builtin_fmaxf(l, -1e30f) : l, rc.y, rc.x);
+            else
+              y[r] = p * rc.x;
           }
-          const int c = wc * 8 + tc * 4 + q;
-          nt_at<uint2>(smem, at(rl, c) + 8 * h) =
-              make_uint2(w[0] | ((uint32_t)w[1] << 16), w[2] | ((uint32_t)w[3] << 16));
+          if (hits) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (rel == tc * 32 + 8 * q + r) y[r] += rc.w;
+          }
+          if (BIAS || edge) {  // forbidden tokens and columns past the last
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if ((BIAS && bz[r] == NEG_INF) || v0 + 4 * h + tc * 32 + 8 * q + r >= in.nA) y[r] = 0.f;
+          }
+          nt_at<uint2>(sq, at(n, tc * 8 + 2 * q + h)) =
+              make_uint2(half2_bits(y[0], y[1]) & keep, half2_bits(y[2], y[3]) & keep);
         }
+      __builtin_amdgcn_sched_barrier(0);
+      if (tp == 0) __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): see run()
+      const int64_t m0 = in.b0 + wp * 128 + tp * 32;
+      const int vb = v0 - a.v0;  // within the block of table rows
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 8 * i + (lane >> 3), c = lane & 7;  // 8 columns of row r
+        const uint2 lo = nt_at<uint2>(sq, at(r, 2 * c)), hi = nt_at<uint2>(sq, at(r, 2 * c + 1));
+        if (m0 + r < a.M && vb + 8 * c < a.Vp)
+          *reinterpret_cast<uint4*>(dz + (m0 + r) * a.lv + vb + 8 * c) = make_uint4(lo.x, lo.y, hi.x, hi.y);
+      }
+      // columns 2 n, 2 n + 1 of 16 rows
+      uint32_t x[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        x[i] = nt_at<uint32_t>(sq, at(16 * h + i, n >> 1) + (n & 1) * 4);
+      if (vb + 2 * n < a.Vp) {
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+          if (m0 + 16 * h + 8 * o >= a.Mp) continue;
+          uint32_t lo[4], hi[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            lo[e] = (x[8 * o + 2 * e] & 0xffffu) | (x[8 * o + 2 * e + 1] << 16);
+            hi[e] = (x[8 * o + 2 * e] >> 16) | (x[8 * o + 2 * e + 1] & 0xffff0000u);
+          }
+          uint16_t* t = dzt + (int64_t)(vb + 2 * n) * a.lm + m0 + 16 * h + 8 * o;
+          *reinterpret_cast<uint4*>(t) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+          *reinterpret_cast<uint4*>(t + a.lm) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    __syncthreads();
   };
-  loop.template run<false>(epi);
-
-  const int64_t vb = in.a0 - a.v0;  // within the block of table rows
-  uint16_t* dz = a.dz + b * a.M * a.lv;
-  uint16_t* dzt = a.dzt + b * a.Vp * a.lm;
-#pragma unroll 4
-  for (int i = threadIdx.x; i < 256 * 32; i += NT_T) {
-    const int rl = i >> 5, c = i & 31;
-    if (in.b0 + rl < a.M && vb + 8 * c < a.Vp)
-      *reinterpret_cast<uint4*>(dz + (in.b0 + rl) * a.lv + vb + 8 * c) = nt_at<uint4>(smem, at(rl, c));
-  }
-#pragma unroll 2
-  for (int i = threadIdx.x; i < 128 * 32; i += NT_T) {
-    const int mo = i & 31, vp = i >> 5;  // 8 positions, 2 table rows
-    if (vb + 2 * vp >= a.Vp || in.b0 + 8 * mo >= a.Mp) continue;
-    uint32_t x[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = nt_at<uint32_t>(smem, at(8 * mo + e, vp >> 2) + (vp & 3) * 4);
-    uint32_t lo[4], hi[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      lo[e] = (x[2 * e] & 0xffffu) | (x[2 * e + 1] << 16);
-      hi[e] = (x[2 * e] >> 16) | (x[2 * e + 1] & 0xffff0000u);
-    }
-    uint16_t* o = dzt + (vb + 2 * vp) * a.lm + in.b0 + 8 * mo;
-    *reinterpret_cast<uint4*>(o) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-    *reinterpret_cast<uint4*>(o + a.lm) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-  }
+  loop.template run<true>(epi);
 }
 
 // ---- the two products of the gradient ----------------------------------------------
@@ -1243,8 +1287,8 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   int ab, bb;
   int64_t inst;
   if (!raster_place(a.grid, blockIdx.x, ab, bb, inst)) return;
-  const int64_t b = inst / a.splits;
-  const int sp = (int)(inst % a.splits);
+  const int b = __builtin_amdgcn_readfirstlane((int)inst / a.splits);
+  const int sp = (int)inst - b * a.splits;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
   NtIn in;
   in.A = a.At + b * a.as;
@@ -1513,10 +1557,16 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       d.Mp = w.Mp;
       d.lv = lv;
       d.lm = lm;
-      d.grid = make_raster((nv + 255) / 256, (a.M + LP_BB - 1) / LP_BB, nb);
+      const int64_t nmb = (a.M + LP_BB - 1) / LP_BB, nvb = (nv + 255) / 256;
+      d.grid = make_raster(score_splits(nmb, nb, nvb, (w.Dk + LP_DC - 1) / LP_DC), nmb, nb);
       const dim3 grid((unsigned)d.grid.blocks());
-      if (a.bias) dz_kernel<DT, true><<<grid, NT_T, 0, s>>>(d);
-      else dz_kernel<DT, false><<<grid, NT_T, 0, s>>>(d);
+      if (a.bias) {
+        if (a.h) dz_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(d);
+        else dz_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(d);
+      } else {
+        if (a.h) dz_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(d);
+        else dz_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(d);
+      }
       if ((e = hipGetLastError()) != hipSuccess) return e;
 
       const bool whole = w.Vc >= a.V;  // one block of table rows

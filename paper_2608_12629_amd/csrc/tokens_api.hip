@@ -44,24 +44,9 @@ struct Taker {
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// At most this many workgroups come of sharing out column blocks or a contraction:
-// two rounds on 256 CUs (contractions) or four (columns).
-constexpr int64_t SCORE_WGS = 1024, OUT_WGS = 512;
+// At most this many workgroups come of sharing out a contraction: two rounds on 256 CUs.
+constexpr int64_t OUT_WGS = 512;
 constexpr int64_t HEAD_SCORES = 1 << 24;  // scores from which alternatives take a head
-
-// Shares of the column blocks: the number with the least rounds of 256 workgroups
-// times what one takes, its blocks and about six stages of filling and emptying.
-int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
-  const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / (nmb * B)));
-  int best = 1;
-  double least = HUGE_VAL;
-  for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
-    const double us = (double)cdiv(make_raster(s, nmb, B).blocks(), 256) *
-                      ((double)(cdiv(nvb, s) * stages) + 6);
-    if (us < least) least = us, best = (int)s;
-  }
-  return best;
-}
 
 LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D, int k) {
   LogprobsWs w{};

@@ -2,6 +2,8 @@
 // translation units of the operators on token tables (include/flashtokens.h).
 #pragma once
 
+#include <algorithm>
+#include <cmath>
 #include <initializer_list>
 
 #include "fkm_internal.h"
@@ -74,6 +76,21 @@ inline Raster make_raster(int64_t na, int64_t nb, int64_t inst) {
     if (r.ga > r.gb) r.ga = (r.ga + 1) / 2;
     else r.gb = (r.gb + 1) / 2;
   }
+}
+// At most this many workgroups come of sharing out the column blocks.
+constexpr int64_t SCORE_WGS = 1024;
+// Shares of the column blocks: the number with the least rounds of 256 workgroups
+// times what one takes, its blocks and about six stages of filling and emptying.
+inline int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
+  const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / (nmb * B)));
+  int best = 1;
+  double least = HUGE_VAL;
+  for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
+    const double us = (double)((make_raster(s, nmb, B).blocks() + 255) / 256) *
+                      ((double)((nvb + s - 1) / s * stages) + 6);
+    if (us < least) least = us, best = (int)s;
+  }
+  return best;
 }
 constexpr int64_t LP_FEW_M = 64;
 struct LogprobsPlan {
