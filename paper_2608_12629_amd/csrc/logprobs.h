@@ -6,8 +6,8 @@
 // One tiled product carries it all, P[a, b] = sum_c A[a, c] B[b, c] with both
 // operands' contraction contiguous: 256 (or 128) rows of A by 256 rows of B to a
 // workgroup of eight waves, each 2 (or 1) x 4 tiles of 32 x 32 x 16 MFMAs.  Stages of
-// 32 elements of both operands go from L2 straight into one of four LDS buffers,
-// two to three stages ahead of the MFMAs, which read them conflict-free from
+// 64 elements of both operands go from L2 straight into one of two LDS buffers, a whole
+// 128-byte line of a row at a time, while the MFMAs read the other conflict-free from
 // swizzled rows.  A's rows lie in a lane's registers and B's across the lanes, so
 // with the table as A a lane holds 32 scores of one position and the softmax's
 // running maximum, sum and weighted sum stay in that lane until the last block.
@@ -28,7 +28,7 @@ constexpr float NEG_INF = -__builtin_inff();
 
 __device__ const uint4 nt_zero = {0, 0, 0, 0};
 
-// L2 -> LDS copies of 16 (or 4) bytes a lane into the wave's slots at `lds`, issued
+// L2 -> LDS copies of 16 bytes a lane into the wave's slots at `lds`, issued
 // by inline assembly so that only the explicit waits below govern them; M0 (the LDS
 // base) is set in the same statement, one wait state before the load reads it.  From
 // a scalar base and 32-bit offsets, or from 64-bit addresses.
@@ -54,12 +54,6 @@ __device__ __forceinline__ void nt_dma16(const void* src, char* lds) {
                : "v"(src), "s"(nt_lds(lds))
                : "memory");
 }
-__device__ __forceinline__ void nt_dma4(const char* base, uint32_t off, char* lds) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1"
-               :
-               : "v"(off), "s"(base), "s"(nt_lds(lds))
-               : "memory");
-}
 
 // Until at most n of this wave's vector memory operations are in flight and its LDS
 // reads are done, then a barrier that leaves the later loads in flight.
@@ -69,22 +63,23 @@ __device__ __forceinline__ void nt_wait_and_sync() {
   asm volatile("s_barrier" ::: "memory");
 }
 
-// Row r of a stage keeps its four 16-byte chunks in slots c ^ swz(r).
-__device__ __forceinline__ int nt_swz(int r) { return ((r >> 1) & 3) ^ ((r >> 3) & 1); }
+// Row r of a stage keeps its eight 16-byte chunks in slots c ^ nt_swz(r): 16 rows' reads
+// of one chunk then meet all 64 banks.
+__device__ __forceinline__ int nt_swz(int r) { return (r >> 1) & 7; }
 
 template <typename T>
 __device__ __forceinline__ T& nt_at(char* base, int off) {
   return *reinterpret_cast<T*>(base + off);
 }
 
-template <int TCW, bool BIAS>
+template <int TCW>
 struct NtSize {
-  static constexpr int BA = 128 * TCW;           // rows of A in a block
-  static constexpr int AB = BA * 64;             // bytes of A in a stage
-  static constexpr int BBY = LP_BB * 64;         // bytes of B
-  static constexpr int STAGE = AB + BBY + (BIAS ? NT_T * 4 : 0);
-  static constexpr int LOADS = TCW + 2 + (BIAS ? 1 : 0);  // loads of a thread in a stage
-  static constexpr int SMEM = 4 * STAGE;
+  static constexpr int BA = 128 * TCW;      // rows of A in a block
+  static constexpr int AB = BA * 128;       // bytes of A in a stage
+  static constexpr int STAGE = AB + LP_BB * 128;
+  static constexpr int LA = BA * 8 / NT_T, LB = LP_BB * 8 / NT_T;  // loads of a thread in a stage
+  static constexpr int LOADS = LA + LB;
+  static constexpr int SMEM = 2 * STAGE;
 };
 
 // The operands of a workgroup: rows a0 .. of A (nblk blocks) by rows b0 .. of B,
@@ -92,7 +87,6 @@ struct NtSize {
 // one (their results are dropped), chunks past c1 as zeros.
 struct NtIn {
   const char *A, *B;
-  const float* bias;  // of A's rows
   int64_t lda, ldb;   // bytes of a row
   int nA, nB, a0, b0, c0, c1, nblk;
 };
@@ -102,25 +96,24 @@ struct NtFrag {
   uint4 a[TCW], b[4];
 };
 
-template <int DT, int TCW, bool BIAS>
+template <int DT, int TCW>
 struct NtLoop {
-  using Z = NtSize<TCW, BIAS>;
+  using Z = NtSize<TCW>;
   NtIn in;
   // the stage to load next: block iblk, stage id of it; each operand's first row and
   // chunk of that stage, and the thread's offsets from it (rows clamped)
   const char *ab, *bb;
-  uint32_t ao[TCW], bo[2], biaso;
+  uint32_t ao[Z::LA], bo[Z::LB];
   int tid, wave, cc, iblk, id, nds;
-  int loff0, loff1, wp, wc;
+  int lo, wp, wc;
   char* smem;
 
   __device__ __forceinline__ void block_rows(int blk) {
-    const int a0 = in.a0 + blk * Z::BA, last = in.nA - 1 - a0, r = tid >> 2;
+    const int a0 = in.a0 + blk * Z::BA, last = in.nA - 1 - a0;
     ab = nt_uniform(in.A + (int64_t)a0 * in.lda + in.c0 * 16);
 #pragma unroll
-    for (int u = 0; u < TCW; ++u)
-      ao[u] = (uint32_t)max(min(r + 128 * u, last), 0) * (uint32_t)in.lda + cc * 16;
-    if constexpr (BIAS) biaso = (uint32_t)min(tid & (Z::BA - 1), max(last, 0)) * 4;
+    for (int u = 0; u < Z::LA; ++u)
+      ao[u] = (uint32_t)max(min((tid >> 3) + 64 * u, last), 0) * (uint32_t)in.lda + cc * 16;
   }
 
   __device__ __forceinline__ void init(const NtIn& i, char* sm) {
@@ -129,17 +122,16 @@ struct NtLoop {
     tid = threadIdx.x;
     wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lane = tid & 63, n = lane & 31, h = lane >> 5;
-    cc = (tid & 3) ^ nt_swz(tid >> 2);
-    nds = (in.c1 - in.c0 + 3) / 4;
+    cc = (tid & 7) ^ nt_swz(tid >> 3);
+    nds = (in.c1 - in.c0 + 7) / 8;
     iblk = id = 0;
     bb = nt_uniform(in.B + (int64_t)in.b0 * in.ldb + in.c0 * 16);
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      bo[u] = (uint32_t)min((tid >> 2) + 128 * u, in.nB - 1 - in.b0) * (uint32_t)in.ldb + cc * 16;
+    for (int u = 0; u < Z::LB; ++u)
+      bo[u] = (uint32_t)min((tid >> 3) + 64 * u, in.nB - 1 - in.b0) * (uint32_t)in.ldb + cc * 16;
     block_rows(0);
     // lane 32 h + n reads row (tile base + n), chunk 2 step + h
-    loff0 = n * 64 + ((0 + h) ^ nt_swz(n)) * 16;
-    loff1 = n * 64 + ((2 + h) ^ nt_swz(n)) * 16;
+    lo = n * 128 + (h ^ nt_swz(n)) * 16;
     wp = wave & 1;   // half of B's rows
     wc = wave >> 1;  // quarter of A's rows
   }
@@ -147,51 +139,42 @@ struct NtLoop {
   // Start the loads of the next stage.
   __device__ __forceinline__ void issue(char* buf) {
     char* dst = buf + wave * 1024;
-    if (in.c0 + id * 4 + 4 <= in.c1) {
+    if (in.c0 + id * 8 + 8 <= in.c1) {
 #pragma unroll
-      for (int u = 0; u < TCW; ++u) nt_dma16(ab, ao[u], dst + u * (NT_T * 16));
+      for (int u = 0; u < Z::LA; ++u) nt_dma16(ab, ao[u], dst + u * (NT_T * 16));
 #pragma unroll
-      for (int u = 0; u < 2; ++u) nt_dma16(bb + id * 64, bo[u], dst + Z::AB + u * (NT_T * 16));
+      for (int u = 0; u < Z::LB; ++u) nt_dma16(bb + id * 128, bo[u], dst + Z::AB + u * (NT_T * 16));
     } else {  // the last stage of a contraction that is no whole number of them
-      const bool have = in.c0 + id * 4 + cc < in.c1;
+      const bool have = in.c0 + id * 8 + cc < in.c1;
 #pragma unroll
-      for (int u = 0; u < TCW; ++u)
+      for (int u = 0; u < Z::LA; ++u)
         nt_dma16(have ? ab + ao[u] : (const char*)&nt_zero, dst + u * (NT_T * 16));
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-        nt_dma16(have ? bb + id * 64 + bo[u] : (const char*)&nt_zero, dst + Z::AB + u * (NT_T * 16));
+      for (int u = 0; u < Z::LB; ++u)
+        nt_dma16(have ? bb + id * 128 + bo[u] : (const char*)&nt_zero, dst + Z::AB + u * (NT_T * 16));
     }
-    if constexpr (BIAS)
-      nt_dma4((const char*)(in.bias + in.a0 + iblk * Z::BA), biaso, buf + Z::AB + Z::BBY + wave * 256);
-    ab += 64;
+    ab += 128;
     if (++id == nds) {
       id = 0;
       block_rows(++iblk);
     }
   }
 
-  __device__ __forceinline__ void read_a(NtFrag<TCW>& f, char* buf, int lo, int tc) {
-    f.a[tc] = nt_at<uint4>(buf, (wc * TCW + tc) * 2048 + lo);
+  __device__ __forceinline__ void read(NtFrag<TCW>& f, char* buf, int i) {  // i-th fragment
+    if (i < TCW) f.a[i < TCW ? i : 0] = nt_at<uint4>(buf, (wc * TCW + i) * 4096);
+    else f.b[i < TCW ? 0 : i - TCW] = nt_at<uint4>(buf, Z::AB + (wp * 4 + i - TCW) * 4096);
   }
-  __device__ __forceinline__ void read_b(NtFrag<TCW>& f, char* buf, int lo, int tp) {
-    f.b[tp] = nt_at<uint4>(buf, Z::AB + (wp * 4 + tp) * 2048 + lo);
-  }
-  __device__ __forceinline__ void read(NtFrag<TCW>& f, char* buf, int lo) {
-#pragma unroll
-    for (int tc = 0; tc < TCW; ++tc) read_a(f, buf, lo, tc);
-#pragma unroll
-    for (int tp = 0; tp < 4; ++tp) read_b(f, buf, lo, tp);
-  }
+  // Step k (16 elements) of a stage's buffer, at this lane's row.
+  __device__ __forceinline__ char* step_at(char* buf, int k) { return buf + (lo ^ (k * 32)); }
 
   // The MFMAs of one 16-element step on `f`, in a fixed order with everything else that
   // the wave has to issue between them: the next step's fragments into `g` from `buf`,
-  // then (LOAD, if there is a stage left to load) the loads of a later stage into
-  // `ahead`.  The matrix cores take 32 cycles an MFMA, so what stands between two of
-  // them is free; in a block of its own, after the barrier and before the MFMAs, it cost
-  // both waves of a SIMD the same idle cycles.
-  template <bool LOAD>
+  // then (if `load`) the loads of a later stage into `ahead`.  The matrix cores take 32
+  // cycles an MFMA, so what stands between two of them is free; in a block of its own,
+  // after the barrier and before the MFMAs, it cost both waves of a SIMD the same idle
+  // cycles.
   __device__ __forceinline__ void step(f32x16 (&acc)[4][TCW], const NtFrag<TCW>& f, NtFrag<TCW>& g,
-                                       char* buf, int lo, char* ahead, bool more) {
+                                       char* buf, char* ahead, bool load) {
     constexpr int N = 4 * TCW, R = TCW + 4;
 #pragma unroll
     for (int m = 0; m < N; ++m) {
@@ -199,54 +182,47 @@ struct NtLoop {
       acc[tp][tc] = mfma32_chunk<DT>(f.a[tc], f.b[tp], acc[tp][tc]);
       __builtin_amdgcn_sched_barrier(0);
       // two reads after each of the first MFMAs (a step has at least 4)
-#pragma unroll
-      for (int i = 2 * m; i < 2 * m + 2; ++i) {
-        if (i < TCW) read_a(g, buf, lo, i);
-        else if (i < R) read_b(g, buf, lo, i - TCW);
-      }
-      if constexpr (LOAD) {
-        if (m == N / 2 && more) issue(ahead);
-      }
+      if (2 * m < R) read(g, buf, 2 * m);
+      if (2 * m + 1 < R) read(g, buf, 2 * m + 1);
+      if (m == N / 2 && load) issue(ahead);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
 
-  // Stage s (its first step's fragments are in f0): read the second step's beside the
-  // first step's MFMAs, wait for stage s + 1, then beside the second step's MFMAs read
-  // stage s + 1's first fragments and start stage s + 3 into the buffer of stage s - 1,
-  // which every wave has finished.  Past the last stage the reads bring values that
-  // nobody uses; one path for all stages keeps the accumulators in their registers.
-  // `landed`: this wave knows that the loads of stage s + 1 are done.
-  __device__ __forceinline__ void stage(int s, int S, bool landed, f32x16 (&acc)[4][TCW],
-                                        NtFrag<TCW>& f0, NtFrag<TCW>& f1) {
-    step<false>(acc, f0, f1, at(s), loff1, nullptr, false);
-    if (landed) nt_wait_and_sync<63>();
-    else if (s + 2 < S) nt_wait_and_sync<Z::LOADS>();
-    else nt_wait_and_sync<0>();
-    step<true>(acc, f1, f0, at(s + 1), loff0, at(s + 3), s + 3 < S);
+  // Stage s, whose first step's fragments are in f0.  Three steps read the next one's
+  // fragments; then every wave has read the stage's buffer, and after a barrier, for
+  // which stage s + 1 has to be there, the last step goes with the first fragments of
+  // stage s + 1 and the loads of stage s + 2 (`load`) into this stage's buffer.  Past the
+  // last stage the reads bring values that nobody uses; one path for all stages keeps
+  // the accumulators in their registers.
+  __device__ __forceinline__ void stage(int s, bool load, f32x16 (&acc)[4][TCW], NtFrag<TCW>& f0,
+                                        NtFrag<TCW>& f1) {
+    char *cur = at(s), *nxt = at(s + 1);
+    step(acc, f0, f1, step_at(cur, 1), nullptr, false);
+    step(acc, f1, f0, step_at(cur, 2), nullptr, false);
+    step(acc, f0, f1, step_at(cur, 3), nullptr, false);
+    nt_wait_and_sync<0>();
+    step(acc, f1, f0, step_at(nxt, 0), cur, load);
   }
-  __device__ __forceinline__ char* at(int s) { return smem + (s & 3) * Z::STAGE; }
+  __device__ __forceinline__ char* at(int s) { return smem + (s & 1) * Z::STAGE; }
 
-  // epi(acc, block, the finished stage's buffer) after each block.  Every wave is past
-  // that stage's barrier, and so has read it; nothing is loaded into it before the next
-  // stage's barrier, which every wave reaches after its epilogue: it is free, but for the
-  // block's bias behind the operands.  STORES: the epilogue waits for the loads in flight
-  // (of the next three stages) before its first store, so that the stages after it need
-  // not: vmcnt counts in issue order, and a wait for loads that were issued after stores
-  // waits for the stores.
-  template <bool STORES, class Epi>
+  // epi(acc, block, scratch) after each block.  SCRATCH: the loads of the stage after the
+  // next, into the buffer of the block's last stage, are put off until the wave is
+  // through with its epilogue, which meanwhile has the parts of that buffer that these
+  // loads of its own will fill: rows of 128 bytes, eight consecutive ones every 8 KiB
+  // (scratch_row).
+  template <bool SCRATCH, class Epi>
   __device__ __forceinline__ void run(Epi&& epi) {
     const int S = in.nblk * nds;
     issue(at(0));
     if (1 < S) issue(at(1));
-    if (2 < S) issue(at(2));
-    if (2 < S) nt_wait_and_sync<2 * Z::LOADS>();
-    else if (1 < S) nt_wait_and_sync<Z::LOADS>();
+    if (1 < S) nt_wait_and_sync<Z::LOADS>();
     else nt_wait_and_sync<0>();
     NtFrag<TCW> f0, f1;
-    read(f0, at(0), loff0);
+#pragma unroll
+    for (int i = 0; i < TCW + 4; ++i) read(f0, step_at(at(0), 0), i);
     f32x16 acc[4][TCW];
-    int s = 0, landed = 0;
+    int s = 0;
     for (int g = 0; g < in.nblk; ++g) {
 #pragma unroll
       for (int tp = 0; tp < 4; ++tp)
@@ -254,12 +230,29 @@ struct NtLoop {
         for (int tc = 0; tc < TCW; ++tc)
 #pragma unroll
           for (int j = 0; j < 16; ++j) acc[tp][tc][j] = 0.f;
-      for (const int end = s + nds; s < end; ++s) stage(s, S, s < landed, acc, f0, f1);
-      epi(acc, g, at(s - 1));
-      if (STORES) landed = s + 2;
+      for (const int end = s + nds; s < end; ++s)
+        stage(s, s + 2 < S && !(SCRATCH && s == end - 1), acc, f0, f1);
+      epi(acc, g, at(s - 1) + wave * 1024);
+      if (SCRATCH && s + 1 < S) issue(at(s - 1));
     }
   }
 };
+// Byte of row r (0 .. 31) of a wave's scratch.
+__device__ __forceinline__ int scratch_row(int r) { return (r >> 3) * (NT_T * 16) + (r & 7) * 128; }
+
+// The offsets of the wave's 64 columns from v0 on, one a lane (0 past the last).
+__device__ __forceinline__ float bias_lane(const float* bias, int v0, int V) {
+  const int v = v0 + (threadIdx.x & 63);
+  return v < V ? bias[v] : 0.f;
+}
+// Those of columns at .. at + 3 (a multiple of 4, different between the half-waves).
+__device__ __forceinline__ f32x4 bias_quad(float lane_bias, int at) {
+  f32x4 x;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+    x[r] = __int_as_float(__builtin_amdgcn_ds_bpermute((at + r) * 4, __float_as_int(lane_bias)));
+  return x;
+}
 
 // ---- softmax statistics ----------------------------------------------------------
 // Of some scores z: m = max (at least -FLT_MAX), s = sum exp(z - m), t = sum
@@ -334,7 +327,7 @@ struct ScoreArgs {
 
 template <int DT, bool BIAS, bool TOPK>
 __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
-  using Z = NtSize<2, BIAS>;
+  using Z = NtSize<2>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   int mb, sp;
   int64_t b;
@@ -345,7 +338,6 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
-  in.bias = BIAS ? a.bias + b * a.V : nullptr;
   in.lda = in.ldb = a.ld;
   in.nA = a.V;
   in.nB = (int)a.rows;
@@ -354,7 +346,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   in.c0 = 0;
   in.c1 = a.chunks;
   in.nblk = blk1 - blk0;
-  NtLoop<DT, 2, BIAS> loop;
+  NtLoop<DT, 2> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   // per row: the target, its score, the bound (in LDS: registers are short)
@@ -371,8 +363,8 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   __syncthreads();
   const float c2 = a.scale * LOG2E;
   auto epi = [&](f32x16(&acc)[4][2], int g, char* scratch) {
-    const float* bias = reinterpret_cast<const float*>(scratch + Z::AB + Z::BBY);
     const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
+    const float bl = BIAS ? bias_lane(a.bias + b * a.V, v0, a.V) : 0.f;
     const bool edge = v0 + 64 > a.V;
     if (BIAS || edge) {  // the scores themselves, with the offsets, into acc
 #pragma unroll
@@ -381,7 +373,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
         for (int q = 0; q < 4; ++q) {
           f32x4 x = {0, 0, 0, 0};
           const int at = tc * 32 + 8 * q + 4 * h;
-          if constexpr (BIAS) x = *reinterpret_cast<const f32x4*>(bias + wc * 64 + at);
+          if constexpr (BIAS) x = bias_quad(bl, at);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             // a forbidden token's score is -inf, whatever its row holds
@@ -454,27 +446,25 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
         const int64_t row = in.b0 + rl;
         const float gm = __builtin_fmaxf(lm, __shfl_xor(lm, 32));
         const bool keep = !a.bound || gm > bound_s[rl];
-        if (tp == 0) __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): see run()
         if (row < a.rows && h == 0 && v0 < a.V)
           a.gmax[(b * a.rows + row) * a.groups + v0 / LP_GROUP] = keep ? gm : NEG_INF;
-        // 32 x 32 scores at a time through the wave's eighth of the finished stage's
+        // 32 x 32 scores at a time through the wave's part of the finished stage's
         // buffer (row n's 16-byte unit c at c ^ (n & 7)), so that whole lines are written:
         // straight from the lanes, 32 bytes of each of 32 rows, they took 2.5 times as long
         const uint64_t kept = __ballot(row < a.rows && keep);
         if (kept) {
           float* zr = a.z + (b * a.rows + in.b0 + wp * 128 + tp * 32) * a.ldz + v0;
-          char* sq = scratch + loop.wave * 4096;
 #pragma unroll
           for (int tc = 0; tc < 2; ++tc) {
             const f32x16& x = acc[tp][tc];
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-              nt_at<f32x4>(sq, n * 128 + (((2 * q + h) ^ (n & 7)) << 4)) =
+              nt_at<f32x4>(scratch, scratch_row(n) + (((2 * q + h) ^ (n & 7)) << 4)) =
                   f32x4{x[4 * q] * zs, x[4 * q + 1] * zs, x[4 * q + 2] * zs, x[4 * q + 3] * zs};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int r = 8 * i + (lane >> 3), c = lane & 7;
-              const f32x4 y = nt_at<f32x4>(sq, r * 128 + ((c ^ (r & 7)) << 4));
+              const f32x4 y = nt_at<f32x4>(scratch, scratch_row(r) + ((c ^ (r & 7)) << 4));
               if (kept >> r & 1) *reinterpret_cast<f32x4*>(zr + r * a.ldz + tc * 32 + 4 * c) = y;
             }
           }
@@ -1089,11 +1079,11 @@ struct DzArgs {
 // dz of 256 positions by a share of the column blocks, in fp16, and its transpose.  The
 // scores come as in score_kernel; with the row's constants c0 = -(h entropy + g) and c1 =
 // -h ln 2 (times DZ_UP), dz = 2^l (c0 + c1 l), l = log2 p one fma of the accumulator, and g
-// more at the target.  32 x 64 values at a time go through the wave's eighth of the
+// more at the target.  32 x 64 values at a time go through the wave's part of the
 // finished stage's buffer, so that lines of both results are written whole.
 template <int DT, bool BIAS, bool ENT>
 __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
-  using Z = NtSize<2, BIAS>;
+  using Z = NtSize<2>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   __shared__ float4 row_s[LP_BB];  // c0, c1, lse in units of log 2, g
   __shared__ int tgt_s[LP_BB];     // -1: none; -2: the row takes no part
@@ -1105,7 +1095,6 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   NtIn in;
   in.A = a.W + b * a.ws;
   in.B = a.X + b * a.xs;
-  in.bias = BIAS ? a.bias + b * a.V : nullptr;
   in.lda = in.ldb = a.ld;
   in.nA = a.v0 + a.nv;
   in.nB = (int)a.M;
@@ -1123,7 +1112,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     tgt_s[r] = rg.active ? rg.target : -2;
   }
   __syncthreads();
-  NtLoop<DT, 2, BIAS> loop;
+  NtLoop<DT, 2> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   const float c2 = a.scale * LOG2E;
@@ -1134,12 +1123,12 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     int lane = threadIdx.x & 63;
     asm volatile("" : "+v"(lane));
     const int n = lane & 31, h = lane >> 5;
-    const float* bias = reinterpret_cast<const float*>(scratch + Z::AB + Z::BBY);
     const int v0 = in.a0 + g * 256 + wc * 64;  // the wave's 64 columns
+    const float bl = BIAS ? bias_lane(a.bias + b * a.V, v0, a.V) : 0.f;
     const bool edge = v0 + 64 > in.nA;
-    char* sq = scratch + loop.wave * 4096;
+    char* sq = scratch;
     // unit u (8 bytes: 4 columns) of row r at u ^ (r & 15)
-    auto at = [&](int r, int u) { return r * 128 + ((u ^ (r & 15)) << 3); };
+    auto at = [&](int r, int u) { return scratch_row(r) + ((u ^ (r & 15)) << 3); };
 #pragma unroll
     for (int tp = 0; tp < 4; ++tp) {
       const int rl = wp * 128 + tp * 32 + n;
@@ -1153,8 +1142,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           f32x4 bz = {0, 0, 0, 0};
-          if constexpr (BIAS)
-            bz = *reinterpret_cast<const f32x4*>(bias + wc * 64 + tc * 32 + 8 * q + 4 * h);
+          if constexpr (BIAS) bz = bias_quad(bl, tc * 32 + 8 * q + 4 * h);
           float y[4];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
@@ -1184,7 +1172,6 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
               make_uint2(half2_bits(y[0], y[1]) & keep, half2_bits(y[2], y[3]) & keep);
         }
       __builtin_amdgcn_sched_barrier(0);
-      if (tp == 0) __builtin_amdgcn_s_waitcnt((7 << 4) | (15 << 8));  // vmcnt(0): see run()
       const int64_t m0 = in.b0 + wp * 128 + tp * 32;
       const int vb = v0 - a.v0;  // within the block of table rows
 #pragma unroll
@@ -1282,7 +1269,7 @@ __device__ __forceinline__ void out_store(const OutArgs& a, int64_t b, int sp, i
 
 template <int DT, int TCW>
 __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
-  using Z = NtSize<TCW, false>;
+  using Z = NtSize<TCW>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   int ab, bb;
   int64_t inst;
@@ -1293,16 +1280,15 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
   NtIn in;
   in.A = a.At + b * a.as;
   in.B = a.Br + b * a.bs;
-  in.bias = nullptr;
   in.lda = in.ldb = a.ld;
   in.nA = a.D;
   in.nB = (int)a.R;
   in.a0 = ab * Z::BA;
   in.b0 = bb * LP_BB;
-  in.c0 = sp * a.per * 4;
-  in.c1 = min(a.chunks, in.c0 + a.per * 4);
+  in.c0 = sp * a.per * 8;
+  in.c1 = min(a.chunks, in.c0 + a.per * 8);
   in.nblk = 1;
-  NtLoop<DT_F16, TCW, false> loop;
+  NtLoop<DT_F16, TCW> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   auto epi = [&](f32x16(&acc)[4][TCW], int, char*) {
@@ -1492,7 +1478,7 @@ hipError_t launch_reduce(const OutArgs& q, int64_t nb, hipStream_t s) {
 template <int DT>
 hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
   const bool narrow = q.D <= 128;
-  const int ba = narrow ? 128 : 256, nst = (q.chunks + 3) / 4;
+  const int ba = narrow ? 128 : 256, nst = (q.chunks + 7) / 8;
   q.per = (nst + splits - 1) / splits;
   q.splits = (nst + q.per - 1) / q.per;
   q.grid = make_raster((q.D + ba - 1) / ba, (q.R + LP_BB - 1) / LP_BB, nb * q.splits);

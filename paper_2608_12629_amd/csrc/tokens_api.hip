@@ -82,9 +82,9 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
 }
 
 // Shares of a contraction of `stages` stages over `tiles` output tiles: enough to
-// fill the chip, of at least 16 stages.
+// fill the chip, of at least 8 stages.
 int out_splits(int64_t tiles, int64_t stages) {
-  return (int)std::max<int64_t>(1, std::min(OUT_WGS / tiles, stages / 16));
+  return (int)std::max<int64_t>(1, std::min(OUT_WGS / tiles, stages / 8));
 }
 
 GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {

@@ -45,8 +45,8 @@ hipError_t launch_embed_grad(const void* G, int gdt, const int32_t* idx, int64_t
 
 // ---- scores against a table (logprobs.h) ----------------------------------------
 // Products are tiled 256 positions x 256 (or 128) table rows; contractions are cut
-// in stages of 32 elements.
-constexpr int LP_BB = 256, LP_DC = 32;
+// in stages of 64 elements.
+constexpr int LP_BB = 256, LP_DC = 64;
 // A scored row's columns come in groups of 64, whose best scores lead to the k best.
 constexpr int LP_GROUP = 64;
 
@@ -80,14 +80,14 @@ inline Raster make_raster(int64_t na, int64_t nb, int64_t inst) {
 // At most this many workgroups come of sharing out the column blocks.
 constexpr int64_t SCORE_WGS = 1024;
 // Shares of the column blocks: the number with the least rounds of 256 workgroups
-// times what one takes, its blocks and about six stages of filling and emptying.
+// times what one takes, its blocks and about three stages of filling and emptying.
 inline int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
   const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / (nmb * B)));
   int best = 1;
   double least = HUGE_VAL;
   for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
     const double us = (double)((make_raster(s, nmb, B).blocks() + 255) / 256) *
-                      ((double)((nvb + s - 1) / s * stages) + 6);
+                      ((double)((nvb + s - 1) / s * stages) + 3);
     if (us < least) least = us, best = (int)s;
   }
   return best;
