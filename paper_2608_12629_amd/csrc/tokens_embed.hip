@@ -4,11 +4,11 @@
 // carries four rows' worth of one 16-byte column.
 //
 // Gradient: dW_v = round(scale * sum over the positions of v of G_m).
-//   1. sort       positions by token, stable
-//   2. zero       rows of dW (tokens without a position stay zero)
-//   3. sums       one wave per slice of consecutive sorted positions and block of
-//                 columns adds each token's rows in fp32 in that order; a run that
-//                 a slice end cuts leaves its part in `carry`
+//   1. sort       positions by token, stable: by counting (rank_kernel) up to 8,192
+//                 positions, else by the update's radix passes
+//   2. clearing   of dW, beside the counting or after the passes
+//   3. sums       slices of consecutive sorted positions add each token's rows in fp32 in
+//                 that order; a run that a slice end cuts leaves its part in `carry`
 //   4. cut runs   the slice where a run starts adds its parts in slice order
 // No atomics on floating-point values: the same bits on every run.
 #include <algorithm>
@@ -37,16 +37,22 @@ template <int DT> struct Tok {
 };
 
 template <int DT, bool VEC>
-__device__ __forceinline__ void load_e(const typename Tok<DT>::T* row, int d, int D,
-                                       float (&v)[Tok<DT>::E]) {
-  constexpr int E = Tok<DT>::E;
-  alignas(16) typename Tok<DT>::T x[E];
+__device__ __forceinline__ uint4 load_raw(const typename Tok<DT>::T* row, int d, int D) {
   if constexpr (VEC) {
-    *reinterpret_cast<uint4*>(x) = *reinterpret_cast<const uint4*>(row + d);
+    return *reinterpret_cast<const uint4*>(row + d);
   } else {
+    constexpr int E = Tok<DT>::E;
+    alignas(16) typename Tok<DT>::T x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = d + e < D ? row[d + e] : typename Tok<DT>::T(0);
+    return *reinterpret_cast<const uint4*>(x);
   }
+}
+template <int DT>
+__device__ __forceinline__ void widen_e(const uint4& raw, float (&v)[Tok<DT>::E]) {
+  constexpr int E = Tok<DT>::E;
+  alignas(16) typename Tok<DT>::T x[E];
+  *reinterpret_cast<uint4*>(x) = raw;
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = Tok<DT>::widen(x[e]);
 }
@@ -95,7 +101,7 @@ __global__ __launch_bounds__(256) void embed_kernel(const typename Tok<DT>::T* _
 #pragma unroll
     for (int u = 0; u < EMB_U; ++u) {
       if (src[u] >= 0) {
-        load_e<DT, VEC>(W + src[u] * D, d, D, v[u]);
+        widen_e<DT>(load_raw<DT, VEC>(W + src[u] * D, d, D), v[u]);
 #pragma unroll
         for (int e = 0; e < E; ++e) v[u][e] *= scale;
       } else {
@@ -129,147 +135,300 @@ hipError_t launch_embed_dt(const void* W, const int32_t* idx, int64_t B, int64_t
 }
 
 // ---- gradient ------------------------------------------------------------------
-constexpr int64_t SUM_SLICE = 32;  // sorted positions per wave
+// 16 bytes of zeros a thread, at byte 16 i (bytes in all).
+__device__ __forceinline__ void zero_at(char* p, int64_t bytes, int64_t i) {
+  if (16 * i + 16 <= bytes) {
+    *reinterpret_cast<uint4*>(p + 16 * i) = make_uint4(0, 0, 0, 0);
+  } else {
+    for (int64_t j = 16 * i; j < bytes; ++j) p[j] = 0;
+  }
+}
+// (HBM takes 7 TB/s from many small workgroups; 4.4 from ones that clear 64 KiB each.)
+__global__ __launch_bounds__(256) void zero_kernel(char* __restrict__ p, int64_t bytes, int64_t from) {
+  zero_at(p, bytes, from + (int64_t)blockIdx.x * 256 + threadIdx.x);
+}
 
-__global__ __launch_bounds__(256) void zero_kernel(char* __restrict__ p, int64_t bytes) {
-  for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 16; i < bytes;
-       i += (int64_t)gridDim.x * 4096) {
-    if (i + 16 <= bytes) {
-      *reinterpret_cast<uint4*>(p + i) = make_uint4(0, 0, 0, 0);
+// Positions sorted by token in one launch: a position's place is the number of positions
+// with a smaller token, or with the same one further ahead.  A workgroup places 16
+// positions; the tokens pass through LDS 4,096 at a time, and each lane counts those of
+// its position over a 64th of them (a read brings four, a compare and an add-with-carry
+// each).  9 us at 4,099 positions, 20 at 8,192; the radix passes 12 us each.  Workgroups past
+// the first `nrank` clear dW.
+constexpr int RANK_CHUNK = 4096, RANK_T = 1024, RANK_P = 16;
+__global__ __launch_bounds__(RANK_T) void rank_kernel(const int32_t* __restrict__ idx, int M, int V,
+                                                      int32_t* __restrict__ keys,
+                                                      int32_t* __restrict__ perm,
+                                                      int32_t* __restrict__ total, int nrank,
+                                                      char* __restrict__ zero, int64_t bytes) {
+  const int tid = threadIdx.x;
+  if ((int)blockIdx.x >= nrank) {
+    const int64_t per = gridDim.x - nrank;
+    zero_at(zero, bytes, (blockIdx.y * per + blockIdx.x - nrank) * RANK_T + tid);
+    return;
+  }
+  constexpr int NONE = 0x7fffffff, P = RANK_P, PARTS = RANK_T / P;
+  __shared__ __attribute__((aligned(16))) int ids[RANK_CHUNK];
+  __shared__ int place[P], valid;
+  const int64_t b = blockIdx.y;
+  idx += b * M;
+  const int pl = tid % P, part = tid / P;  // the position and part of this lane
+  const int p0 = blockIdx.x * P, p = p0 + pl;
+  const int id = p < M ? idx[p] : -1;
+  if (tid < P) place[tid] = 0;
+  if (tid == 0) valid = 0;
+  int cnt = 0;
+  for (int c0 = 0; c0 < M; c0 += RANK_CHUNK) {
+    __syncthreads();
+    int nv = 0;
+#pragma unroll
+    for (int u = 0; u < RANK_CHUNK / RANK_T; ++u) {
+      const int j = c0 + u * RANK_T + tid;
+      const int v = j < M ? idx[j] : -1;
+      const bool ok = (unsigned)v < (unsigned)V;
+      ids[u * RANK_T + tid] = ok ? v : NONE;
+      nv += __popcll(__ballot(ok));
+    }
+    if (blockIdx.x == 0 && (tid & 63) == 0) atomicAdd(&valid, nv);
+    __syncthreads();
+    // this lane's tokens: every PARTS-th four
+    const int4* q = reinterpret_cast<const int4*>(ids);
+    constexpr int N = RANK_CHUNK / 4 / PARTS;
+    if (c0 + RANK_CHUNK <= p0 || c0 > p0) {  // all ahead of the positions, or none
+      const int lim = c0 <= p0 ? id + 1 : id;
+#pragma unroll 8
+      for (int i = 0; i < N; ++i) {
+        const int4 v = q[i * PARTS + part];
+        cnt += v.x < lim;
+        cnt += v.y < lim;
+        cnt += v.z < lim;
+        cnt += v.w < lim;
+      }
     } else {
-      for (int64_t j = i; j < bytes; ++j) p[j] = 0;
+#pragma unroll 8
+      for (int i = 0; i < N; ++i) {
+        const int4 v = q[i * PARTS + part];
+        const int ahead = p - (c0 + 4 * (i * PARTS + part));  // tokens of this four ahead of p
+        cnt += v.x < id + (ahead > 0);
+        cnt += v.y < id + (ahead > 1);
+        cnt += v.z < id + (ahead > 2);
+        cnt += v.w < id + (ahead > 3);
+      }
     }
   }
+  atomicAdd(&place[pl], cnt);
+  __syncthreads();
+  if (tid < P && (unsigned)id < (unsigned)V) {
+    keys[b * M + place[tid]] = id;
+    perm[b * M + place[tid]] = p;
+  }
+  if (blockIdx.x == 0 && tid == 0) total[b] = valid;
 }
 
 // The row of token v gets `acc` (times scale; added to what it holds).
 template <int WT, int E, bool VEC>
-__device__ __forceinline__ void put_row(typename Tok<WT>::T* row, int d, int D, float (&acc)[E],
-                                        float scale, bool accumulate) {
+__device__ __forceinline__ void put_row(typename Tok<WT>::T* row, int d, int D,
+                                        const float (&acc)[E], float scale, bool accumulate) {
+  float v[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] *= scale;
+  for (int e = 0; e < E; ++e) v[e] = acc[e] * scale;
   if (accumulate) {
-    using T = typename Tok<WT>::T;
 #pragma unroll
     for (int e = 0; e < E; ++e)
-      if (VEC || d + e < D) acc[e] += Tok<WT>::widen((T)row[d + e]);
+      if (VEC || d + e < D) v[e] += Tok<WT>::widen(row[d + e]);
   }
-  store_e<WT, E, VEC>(row, d, D, acc);
+  store_e<WT, E, VEC>(row, d, D, v);
 }
 
-// One wave per slice and block of LPR column chunks; 64 / LPR rows in a step,
-// added up at each run's end in a fixed order.
+// lpr lanes (one 16-byte column each) take a slice of `slice` sorted positions: all its
+// rows are on their way, eight at a time, whatever tokens they belong to, and are added
+// in order; where the token changes, the sum goes to its row of dW, or to `carry` (the
+// slice's first or last) if the token's run goes on beyond the slice.
+// Slices of 16 positions, or up to 128 while that leaves 4,096 waves: fewer cut runs.
+int sum_lanes(int64_t chunks) {
+  int lpr = 1;
+  while (lpr < 64 && lpr < chunks) lpr *= 2;
+  return lpr;
+}
+constexpr int64_t SUM_MIN = 16, SUM_MAX = 128;
+int64_t sum_slice(int64_t B, int64_t M, int64_t chunks) {
+  const int64_t lanes = sum_lanes(chunks) * ((chunks + 63) / 64);  // of a slice, all columns
+  int64_t slice = SUM_MIN;
+  while (slice < SUM_MAX && B * M / (2 * slice) * lanes >= 4096 * 64) slice *= 2;
+  return slice;
+}
 template <int DT, int WT, bool VEC>
 __global__ __launch_bounds__(256) void embed_sums_kernel(
     const typename Tok<DT>::T* __restrict__ G, const int32_t* __restrict__ keys,
     const int32_t* __restrict__ perm, const int32_t* __restrict__ total, int64_t M, int V, int D,
-    int lpr, int nslices, float scale, int accumulate, typename Tok<WT>::T* __restrict__ dW,
-    float* __restrict__ carry) {
-  constexpr int E = Tok<DT>::E, U = 4;
-  const int lane = threadIdx.x & 63;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t b = blockIdx.z;
-  const int64_t n = total[b], j0 = w * SUM_SLICE;
-  if (j0 >= n) return;
-  const int cnt = (int)min<int64_t>(n - j0, SUM_SLICE);
+    int lpr, int slice, int nslices, float scale, int ncols, int accumulate,
+    typename Tok<WT>::T* __restrict__ dW, float* __restrict__ carry) {
+  constexpr int E = Tok<DT>::E, U = 8;
+  const int64_t b = blockIdx.y, n = total[b];
+  const int64_t w = ((int64_t)(blockIdx.x / ncols) * 256 + threadIdx.x) / lpr;
+  const int64_t j0 = w * slice;
+  // column blocks side by side: one of them at a time, over all rows, would meet only the
+  // memory channels of that part of a row
+  const int d = (blockIdx.x % ncols * lpr + threadIdx.x % lpr) * E;
+  if (j0 >= n || d >= D) return;
+  const int cnt = (int)min<int64_t>(n - j0, slice);
   keys += b * M + j0;
   perm += b * M + j0;
   G += b * M * D;
   dW += b * V * D;
-  // the slice's entries, one a lane; `starts`: the lanes where a run begins
-  const int kl = lane < cnt ? keys[lane] : -1, pl = lane < cnt ? perm[lane] : 0;
+  float* c = carry + (b * nslices + w) * 2 * D;
   const int before = j0 > 0 ? keys[-1] : -1, after = j0 + cnt < n ? keys[cnt] : -1;
-  const int kprev = __shfl_up(kl, 1);
-  const uint64_t starts = __ballot(lane < cnt && (lane == 0 || kl != kprev));
-  const int d = (blockIdx.y * lpr + lane % lpr) * E, r = lane / lpr, rpw = 64 / lpr;
-  int pos = 0;
-  while (pos < cnt) {
-    const int key = __shfl(kl, pos);
-    const uint64_t rest = (starts >> pos) >> 1;
-    const int end = rest ? pos + 1 + (int)__builtin_ctzll(rest) : cnt;
-    float acc[E];
+  int key = keys[0];
+  bool head = before == key;  // the run began in an earlier slice
+  float acc[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = 0.f;
-    for (int j = pos; j < end; j += U * rpw) {
-      float v[U][E];
+  for (int e = 0; e < E; ++e) acc[e] = 0.f;
+  auto flush = [&](bool tail) {
+    if (head || tail) {
+      float* o = c + (head ? 0 : D);
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int jj = j + u * rpw + r;
-        const int64_t p = __shfl(pl, jj & 63);
-        if (jj < end && d < D) {
-          load_e<DT, VEC>(G + p * D, d, D, v[u]);
-        } else {
+      for (int e = 0; e < E; ++e)
+        if (VEC || d + e < D) o[d + e] = acc[e];
+    } else {
+      put_row<WT, E, VEC>(dW + (int64_t)key * D, d, D, acc, scale, accumulate);
+    }
+  };
+  for (int i0 = 0; i0 < cnt; i0 += U) {
+    int k[U];
+    uint4 raw[U];
 #pragma unroll
-          for (int e = 0; e < E; ++e) v[u][e] = 0.f;
-        }
+    for (int u = 0; u < U; ++u) k[u] = keys[min(i0 + u, cnt - 1)];
+#pragma unroll
+    for (int u = 0; u < U; ++u)  // past the last one it again: no branch around a load
+      raw[u] = load_raw<DT, VEC>(G + (int64_t)perm[min(i0 + u, cnt - 1)] * D, d, D);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u >= cnt) break;
+      if (k[u] != key) {
+        flush(false);
+        key = k[u];
+        head = false;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = 0.f;
       }
+      float v[E];
+      widen_e<DT>(raw[u], v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += v[e];
+    }
+  }
+  flush(after == key);
+}
+
+// The slice in which a cut run starts adds the run's parts in slice order, one wave per
+// slice and 64 column chunks.  Runs over more than CUT_LONG slices (a token that a tenth
+// of all positions hold) are then shared by the workgroup's 16 waves.
+constexpr int CUT_T = 1024, CUT_LONG = 64;
+template <int WT, int E, bool VEC>
+__global__ __launch_bounds__(CUT_T) void embed_cut_kernel(
+    const int32_t* __restrict__ keys, const int32_t* __restrict__ total, int64_t M, int V, int D,
+    int slice, int nslices, float scale, int accumulate, const float* __restrict__ carry,
+    typename Tok<WT>::T* __restrict__ dW) {
+  constexpr int W = CUT_T / 64;
+  __shared__ float part[W][64 * E];
+  __shared__ int long_more[W];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t w0 = (int64_t)blockIdx.x * W, b = blockIdx.z;
+  const int64_t n = total[b];
+  if ((w0 + 1) * slice >= n) return;  // nothing after the first slice
+  keys += b * M;
+  const int d = (blockIdx.y * 64 + lane) * E;
+  carry += b * nslices * 2 * D + d;
+  // adds parts i0 + 1 .. i1 (the slices after w), all on their way eight at a time
+  auto add = [&](float (&acc)[E], int64_t w, int i0, int i1) {
+    constexpr int U = 8;
+    const float* c = carry + w * 2 * D;
+    for (; i0 < i1; i0 += U) {
+      float v[U][E];
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] += v[u][e];
-    }
-    for (int m = lpr; m < 64; m <<= 1)
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] += __shfl_xor(acc[e], m);
-    const bool head = pos == 0 && before == key;  // began in an earlier slice
-    const bool tail = end == cnt && after == key;  // goes on in the next
-    if (r == 0 && d < D) {
-      if (head || tail) {
-        float* c = carry + ((b * nslices + w) * 2 + (head ? 0 : 1)) * D;
-#pragma unroll
         for (int e = 0; e < E; ++e)
-          if (VEC || d + e < D) c[d + e] = acc[e];
-      } else {
-        put_row<WT, E, VEC>(dW + (int64_t)key * D, d, D, acc, scale, accumulate);
+          v[u][e] = VEC || d + e < D ? c[(int64_t)min(i0 + u + 1, i1) * 2 * D + e] : 0.f;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (i0 + u >= i1) break;
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += v[u][e];
       }
     }
-    pos = end;
-  }
-}
-
-// The slice in which a cut run starts adds the run's parts in slice order.
-template <int WT, int E, bool VEC>
-__global__ __launch_bounds__(256) void embed_cut_kernel(
-    const int32_t* __restrict__ keys, const int32_t* __restrict__ total, int64_t M, int V, int D,
-    int nslices, float scale, int accumulate, const float* __restrict__ carry,
-    typename Tok<WT>::T* __restrict__ dW) {
-  const int64_t w = blockIdx.x, b = blockIdx.z;
-  const int64_t n = total[b], j0 = w * SUM_SLICE, j1 = j0 + SUM_SLICE;
-  if (j1 >= n) return;  // nothing after this slice
-  keys += b * M;
-  const int key = keys[j1 - 1];
-  if (keys[j1] != key || (j0 > 0 && keys[j0 - 1] == key)) return;  // not cut, or began earlier
-  const int d = (blockIdx.y * 256 + threadIdx.x) * E;
-  if (d >= D) return;
-  const float* c = carry + (b * nslices + w) * 2 * D;
-  float acc[E];
+  };
+  auto first = [&](float (&acc)[E], int64_t w) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = VEC || d + e < D ? c[D + d + e] : 0.f;
-  for (int64_t j = j1; j < n && keys[j] == key; j += SUM_SLICE) {
-    c += 2 * D;
-#pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] += VEC || d + e < D ? c[d + e] : 0.f;
+    for (int e = 0; e < E; ++e) acc[e] = VEC || d + e < D ? carry[w * 2 * D + D + e] : 0.f;
+  };
+  {
+    const int64_t w = w0 + wave, j0 = w * slice, j1 = j0 + slice;
+    int more = 0;  // the slices that this slice's last run goes on into
+    if (j1 < n && keys[j1] == keys[j1 - 1] && (j0 == 0 || keys[j0 - 1] != keys[j1 - 1])) {
+      const int key = keys[j1 - 1];
+      for (;;) {
+        const int64_t j = j1 + (int64_t)(more + lane) * slice;
+        const uint64_t on = ~__ballot(j < n && keys[j] == key);
+        if (on) {
+          more += (int)__builtin_ctzll(on);
+          break;
+        }
+        more += 64;
+      }
+      if (more <= CUT_LONG && d < D) {
+        float acc[E];
+        first(acc, w);
+        add(acc, w, 0, more);
+        put_row<WT, E, VEC>(dW + (b * V + key) * D, d, D, acc, scale, accumulate);
+      }
+    }
+    if (lane == 0) long_more[wave] = more > CUT_LONG ? more : 0;
   }
-  put_row<WT, E, VEC>(dW + (b * V + key) * D, d, D, acc, scale, accumulate);
+  __syncthreads();
+  for (int i = 0; i < W; ++i) {
+    const int more = long_more[i];
+    if (!more) continue;
+    float acc[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+    if (d < D) {
+      if (wave == 0) first(acc, w0 + i);
+      add(acc, w0 + i, more * wave / W, more * (wave + 1) / W);
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) part[wave][e * 64 + lane] = acc[e];
+    __syncthreads();
+    if (wave == 0 && d < D) {
+      for (int q = 1; q < W; ++q)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] += part[q][e * 64 + lane];
+      const int key = keys[(w0 + i + 1) * slice - 1];
+      put_row<WT, E, VEC>(dW + (b * V + key) * D, d, D, acc, scale, accumulate);
+    }
+    __syncthreads();
+  }
 }
 
 template <int DT, int WT, bool VEC>
 hipError_t launch_sums_dt(const void* G, int64_t B, int64_t M, int64_t V, int64_t D, float scale,
                           bool accumulate, void* dW, const EmbedGradWs& w, hipStream_t s) {
   constexpr int E = Tok<DT>::E;
-  const int64_t chunks = (D + E - 1) / E, nslices = (M + SUM_SLICE - 1) / SUM_SLICE;
-  int lpr = 1;
-  while (lpr < 64 && lpr < chunks) lpr *= 2;
+  const int64_t chunks = (D + E - 1) / E, slice = sum_slice(B, M, chunks);
+  const int64_t nslices = (M + slice - 1) / slice;
+  const int lpr = sum_lanes(chunks);
   using T = typename Tok<WT>::T;
+  const int64_t ncols = (chunks + lpr - 1) / lpr;
   embed_sums_kernel<DT, WT, VEC>
-      <<<dim3((unsigned)((nslices + 3) / 4), (unsigned)((chunks + lpr - 1) / lpr), (unsigned)B), 256,
-         0, s>>>((const typename Tok<DT>::T*)G, w.sort.keys[0], w.sort.vals[0], w.sort.total, M,
-                 (int)V, (int)D, lpr, (int)nslices, scale, accumulate, (T*)dW, w.carry);
+      <<<dim3((unsigned)((nslices * lpr + 255) / 256 * ncols), (unsigned)B), 256, 0, s>>>(
+          (const typename Tok<DT>::T*)G, w.sort.keys[0], w.sort.vals[0], w.sort.total, M, (int)V,
+          (int)D, lpr, (int)slice, (int)nslices, scale, (int)ncols, accumulate, (T*)dW, w.carry);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || nslices == 1) return e;
   embed_cut_kernel<WT, E, VEC>
-      <<<dim3((unsigned)nslices, (unsigned)((chunks + 255) / 256), (unsigned)B), 256, 0, s>>>(
-          w.sort.keys[0], w.sort.total, M, (int)V, (int)D, (int)nslices, scale, accumulate, w.carry,
+      <<<dim3((unsigned)((nslices + CUT_T / 64 - 1) / (CUT_T / 64)), (unsigned)((chunks + 63) / 64),
+              (unsigned)B), CUT_T, 0, s>>>(
+          w.sort.keys[0], w.sort.total, M, (int)V, (int)D, (int)slice, (int)nslices, scale,
+          accumulate, w.carry,
           (T*)dW);
   return hipGetLastError();
 }
@@ -301,7 +460,6 @@ EmbedGradWs embed_grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_
     return r;
   };
   const int64_t chunks = (M + RADIX_CHUNK - 1) / RADIX_CHUNK;
-  const int64_t nslices = (M + SUM_SLICE - 1) / SUM_SLICE;
   for (int i = 0; i < 2; ++i) {
     w.sort.keys[i] = (int32_t*)take((size_t)(B * M) * 4);
     w.sort.vals[i] = (int32_t*)take((size_t)(B * M) * 4);
@@ -309,7 +467,8 @@ EmbedGradWs embed_grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_
   w.sort.hist = (int32_t*)take((size_t)(B * RADIX_MAX_R * chunks) * 4);
   w.sort.bins = (int32_t*)take((size_t)(B * RADIX_MAX_R) * 4);
   w.sort.total = (int32_t*)take((size_t)B * 4);
-  w.carry = (float*)take((size_t)(B * nslices * 2 * D) * 4);
+  // slices of at least SUM_MIN positions
+  w.carry = (float*)take((size_t)(B * ((M + SUM_MIN - 1) / SUM_MIN) * 2 * D) * 4);
   w.total = o;
   return w;
 }
@@ -317,13 +476,25 @@ EmbedGradWs embed_grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_
 hipError_t launch_embed_grad(const void* G, int gdt, const int32_t* idx, int64_t B, int64_t M,
                              int64_t V, int64_t D, float scale, bool accumulate, void* dW, int wdt,
                              const EmbedGradWs& w, hipStream_t s) {
-  hipError_t e = launch_token_sort(idx, B, M, V, w.sort, s);
-  if (e != hipSuccess) return e;
-  if (!accumulate) {
-    const int64_t bytes = B * V * D * dt_bytes(wdt);
-    zero_kernel<<<dim3((unsigned)std::min<int64_t>((bytes + 4095) / 4096, MAX_BLOCKS)), 256, 0, s>>>((char*)dW, bytes);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  const int64_t bytes = accumulate ? 0 : B * V * D * dt_bytes(wdt);
+  hipError_t e;
+  if (B * M * M <= (int64_t)1 << 26 && M <= 8192) {  // see rank_kernel
+    const int64_t nrank = (M + RANK_P - 1) / RANK_P, per = RANK_T * 16 * B;
+    const int64_t nzero = (bytes + per - 1) / per;
+    rank_kernel<<<dim3((unsigned)(nrank + nzero), (unsigned)B), RANK_T, 0, s>>>(
+        idx, (int)M, (int)V, w.sort.keys[0], w.sort.vals[0], w.sort.total, (int)nrank, (char*)dW,
+        bytes);
+    e = hipGetLastError();
+  } else {
+    e = launch_token_sort(idx, B, M, V, w.sort, s);
+    constexpr int64_t most = MAX_BLOCKS * 256;  // 16-byte pieces of a launch
+    for (int64_t from = 0; e == hipSuccess && from * 16 < bytes; from += most) {
+      const int64_t n = std::min<int64_t>((bytes + 15) / 16 - from, most);
+      zero_kernel<<<dim3((unsigned)((n + 255) / 256)), 256, 0, s>>>((char*)dW, bytes, from);
+      e = hipGetLastError();
+    }
   }
+  if (e != hipSuccess) return e;
   if (gdt == DT_F32)
     return launch_sums_wt<DT_F32, DT_F32>(G, B, M, V, D, scale, accumulate, dW, w, s);
   if (gdt == DT_BF16)
