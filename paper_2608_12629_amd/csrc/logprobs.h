@@ -883,87 +883,104 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
 // the largest gs) and W times what brings their largest value just below 2^14, where
 // fp16 holds every bf16 or fp16 value down to 2^-28 of that exactly.
 constexpr float DZ_UP = 2048.f;
-constexpr int STATS_WGS = 256;  // workgroups of an instance's statistics
 
 // What each position's gradient needs, and the largest gs and magnitudes: X's of the
-// rows that take part, W's of the tokens that do.  One wave per row.
+// rows that take part, W's of the tokens that do.  A workgroup goes over blocks of `rb`
+// rows (about 64 KiB) of X, or past the first `nx` workgroups of W: first a thread per
+// row, then all threads through the rows' 16-byte chunks.
 template <int DT>
 __global__ __launch_bounds__(512) void grad_rows_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
     const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
-    const float* __restrict__ h, const float* __restrict__ bias, int64_t M, int V, int D,
+    const float* __restrict__ h, const float* __restrict__ bias, int64_t M, int V, int D, int rb, int nx,
     RowGrad* __restrict__ out, float4* __restrict__ stats) {
-  __shared__ float sh[8][3];
+  __shared__ float sh[8][2];
+  __shared__ bool part[512];
   const int64_t b = blockIdx.y;
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, nw = gridDim.x * 8;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const bool is_x = (int)blockIdx.x < nx;
+  const int64_t rows = is_x ? M : V, nblk = is_x ? nx : gridDim.x - nx;
+  const uint16_t* in = (is_x ? X : W) + b * rows * D;
   float gsmax = 0.f;
-  uint32_t mx = 0, mw = 0;  // magnitudes' bits, which order as the values do
+  uint32_t mag = 0;  // the largest magnitude's bits, which order as the values do
   constexpr uint32_t FIN = DT == DT_BF16 ? 0x7f7f : 0x7bff;  // the largest finite one
-  auto row_max = [&](const uint16_t* p, uint32_t m) {
-    auto one = [&](uint32_t v) {
-      v &= 0x7fffu;
-      return v > FIN ? 0u : v;
-    };
+  auto one = [&](uint32_t v) {
+    v &= 0x7fffu;
+    return v > FIN ? 0u : v;
+  };
+  for (int64_t r0 = (is_x ? blockIdx.x : blockIdx.x - nx) * (int64_t)rb; r0 < rows; r0 += nblk * rb) {
+    const int nr = (int)min<int64_t>(rb, rows - r0);
+    if (tid < nr) {
+      if (is_x) {
+        const int64_t i = b * M + r0 + tid;
+        RowGrad r;
+        const int t = target[i];
+        const bool ok = (unsigned)t < (unsigned)V;
+        r.target = ok && (!bias || bias[b * V + (ok ? t : 0)] != NEG_INF) ? t : -1;
+        r.lse = lse[i];
+        r.g = r.target >= 0 ? g[i] : 0.f;
+        r.h = h ? h[i] : 0.f;
+        r.ent = h ? ent[i] : 0.f;
+        r.active = r.lse != NEG_INF && (r.g != 0.f || r.h != 0.f);
+        r.gs = 1.f;
+        r.pad = 0;
+        const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
+        if (r.active && big <= __FLT_MAX__) {
+          int e;
+          (void)frexpf(big, &e);
+          e = min(max(e, -120), 120);
+          r.gs = ldexpf(1.f, e);
+          r.g *= ldexpf(1.f, -e);
+          r.h *= ldexpf(1.f, -e);
+        }
+        out[i] = r;
+        part[tid] = r.active;
+        if (r.active) gsmax = __builtin_fmaxf(gsmax, r.gs);
+      } else {
+        part[tid] = !bias || bias[b * V + r0 + tid] != NEG_INF;
+      }
+    }
+    __syncthreads();
+    const uint16_t* p = in + r0 * D;
     if (D % 8 == 0) {
-      for (int d = lane * 8; d < D; d += 512) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p + d);
-        const uint32_t x[4] = {q.x, q.y, q.z, q.w};
+      const int rc = D / 8, n = nr * rc;
+      for (int i0 = tid; i0 < n; i0 += 4 * 512) {
+        uint4 q[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) m = max(m, max(one(x[e]), one(x[e] >> 16)));
+        for (int u = 0; u < 4; ++u)
+          q[u] = *reinterpret_cast<const uint4*>(p + (int64_t)min(i0 + u * 512, n - 1) * 8);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const uint32_t x[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+          uint32_t m = 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) m = max(m, max(one(x[e]), one(x[e] >> 16)));
+          mag = max(mag, part[min(i0 + u * 512, n - 1) / rc] ? m : 0u);
+        }
       }
     } else {
-      for (int d = lane; d < D; d += 64) m = max(m, one(p[d]));
+      for (int i = tid; i < nr * D; i += 512)
+        if (part[i / D]) mag = max(mag, one(p[i]));
     }
-    return m;
-  };
-  for (int64_t m = blockIdx.x * 8 + w; m < M; m += nw) {
-    const int64_t i = b * M + m;
-    RowGrad r;
-    const int t = target[i];
-    r.target = (unsigned)t < (unsigned)V && (!bias || bias[b * V + t] != NEG_INF) ? t : -1;
-    r.lse = lse[i];
-    r.g = r.target >= 0 ? g[i] : 0.f;
-    r.h = h ? h[i] : 0.f;
-    r.ent = h ? ent[i] : 0.f;
-    r.active = r.lse != NEG_INF && (r.g != 0.f || r.h != 0.f);
-    r.gs = 1.f;
-    r.pad = 0;
-    const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
-    if (r.active && big <= __FLT_MAX__) {
-      int e;
-      (void)frexpf(big, &e);
-      e = min(max(e, -120), 120);
-      r.gs = ldexpf(1.f, e);
-      r.g *= ldexpf(1.f, -e);
-      r.h *= ldexpf(1.f, -e);
-    }
-    if (lane == 0) out[i] = r;
-    if (r.active) {
-      gsmax = __builtin_fmaxf(gsmax, r.gs);
-      mx = row_max(X + i * D, mx);
-    }
+    __syncthreads();
   }
-  for (int v = blockIdx.x * 8 + w; v < V; v += nw)
-    if (!bias || bias[b * V + v] != NEG_INF) mw = row_max(W + (b * V + v) * D, mw);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    mx = max(mx, (uint32_t)__shfl_xor((int)mx, d));
-    mw = max(mw, (uint32_t)__shfl_xor((int)mw, d));
+    mag = max(mag, (uint32_t)__shfl_xor((int)mag, d));
+    gsmax = __builtin_fmaxf(gsmax, __shfl_xor(gsmax, d));
   }
   if (lane == 0) {
     sh[w][0] = gsmax;
-    sh[w][1] = Elem<DT>::widen((uint16_t)mx);
-    sh[w][2] = Elem<DT>::widen((uint16_t)mw);
+    sh[w][1] = Elem<DT>::widen((uint16_t)mag);
   }
   __syncthreads();
-  if (threadIdx.x == 0) {
-    float4 o = make_float4(0, 0, 0, 0);
+  if (tid == 0) {
+    float gm = 0.f, m = 0.f;
     for (int i = 0; i < 8; ++i) {
-      o.x = __builtin_fmaxf(o.x, sh[i][0]);
-      o.y = __builtin_fmaxf(o.y, sh[i][1]);
-      o.z = __builtin_fmaxf(o.z, sh[i][2]);
+      gm = __builtin_fmaxf(gm, sh[i][0]);
+      m = __builtin_fmaxf(m, sh[i][1]);
     }
-    stats[b * gridDim.x + blockIdx.x] = o;
+    stats[b * gridDim.x + blockIdx.x] = make_float4(gm, is_x ? m : 0.f, is_x ? 0.f : m, 0.f);
   }
 }
 
@@ -974,25 +991,22 @@ __device__ __forceinline__ float up_to_2_14(float m) {
   (void)frexpf(m, &e);
   return ldexpf(1.f, min(14 - e, 126));
 }
-// scales[b] = (largest gs, factor of X, factor of W).
-__global__ __launch_bounds__(64) void grad_scales_kernel(const float4* __restrict__ stats, int n,
-                                                         float4* __restrict__ scales) {
-  const int64_t b = blockIdx.x;
+// (largest gs, factor of X, factor of W) from n statistics, by 256 threads.
+__device__ __forceinline__ float4 grad_scales(const float4* stats, int n, float4* sh) {
   float4 o = make_float4(0, 0, 0, 0);
-  for (int i = threadIdx.x; i < n; i += 64) {
-    const float4 s = stats[b * n + i];
+  auto take = [&](const float4& s) {
     o.x = __builtin_fmaxf(o.x, s.x);
     o.y = __builtin_fmaxf(o.y, s.y);
     o.z = __builtin_fmaxf(o.z, s.z);
-  }
+  };
+  for (int i = threadIdx.x; i < n; i += 256) take(stats[i]);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    o.x = __builtin_fmaxf(o.x, __shfl_xor(o.x, d));
-    o.y = __builtin_fmaxf(o.y, __shfl_xor(o.y, d));
-    o.z = __builtin_fmaxf(o.z, __shfl_xor(o.z, d));
-  }
-  if (threadIdx.x == 0)
-    scales[b] = make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_14(o.y), up_to_2_14(o.z), 0.f);
+  for (int d = 1; d < 64; d <<= 1)
+    take(make_float4(__shfl_xor(o.x, d), __shfl_xor(o.y, d), __shfl_xor(o.z, d), 0.f));
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = o;
+  __syncthreads();
+  for (int i = 0; i < 4; ++i) take(sh[i]);
+  return make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_14(o.y), up_to_2_14(o.z), 0.f);
 }
 
 // Transposed fp16 copies: in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance, times a
@@ -1010,16 +1024,18 @@ struct CopyJob {
 };
 template <int DT>
 __global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
-                                                   const float4* __restrict__ scales) {
+                                                   const float4* __restrict__ stats, int nstats,
+                                                   float4* __restrict__ scales) {
+  __shared__ float4 sh[4];
   constexpr int LD = 33;  // pairs from column to column: no conflicts on writes
   __shared__ uint32_t tile[64 * LD];
   const bool is_x = (int)blockIdx.x < x.tiles;
   const CopyJob j = is_x ? x : w;
   const int64_t b = blockIdx.z, rt = (int64_t)((int)blockIdx.x - (is_x ? 0 : x.tiles)) * 64;
   const int ct = blockIdx.y * 64, t = threadIdx.x;
-  const float4 sc = scales[b];
-#pragma unroll
-  for (int u = 0; u < 1; ++u) {
+  const float4 sc = grad_scales(stats + b * nstats, nstats, sh);
+  if (blockIdx.x == 0 && blockIdx.y == 0 && t == 0) scales[b] = sc;  // for the products
+  {
     const int c8 = t % 8, rp = t / 8;  // 8 columns of rows 2 rp, 2 rp + 1
     uint16_t v[2][8];
 #pragma unroll
@@ -1267,13 +1283,16 @@ __device__ __forceinline__ void out_store(const OutArgs& a, int64_t b, int sp, i
   }
 }
 
+// (Both products in one launch: the workgroups past the first np are q's.)
 template <int DT, int TCW>
-__global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
+__global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int np) {
   using Z = NtSize<TCW>;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
+  const bool is_p = (int)blockIdx.x < np;
+  const OutArgs a = is_p ? p : q;
   int ab, bb;
   int64_t inst;
-  if (!raster_place(a.grid, blockIdx.x, ab, bb, inst)) return;
+  if (!raster_place(a.grid, blockIdx.x - (is_p ? 0 : np), ab, bb, inst)) return;
   const int b = __builtin_amdgcn_readfirstlane((int)inst / a.splits);
   const int sp = (int)inst - b * a.splits;
   const int lane = threadIdx.x & 63, n = lane & 31, h = lane >> 5;
@@ -1326,12 +1345,14 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs a) {
 // out[b, r, d] = the sum over the shares of part[b, s, r, d] in their order, times its
 // factor; eight results a thread.
 template <int DT>
-__global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs a, int64_t nb) {
+__global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, int np, int64_t nb) {
+  const bool is_p = (int)blockIdx.x < np;
+  const OutArgs a = is_p ? p : q;
   const int dc = (a.D + 7) / 8;
-  const int64_t n = nb * a.R * dc;
+  const int64_t n = nb * a.R * dc, step = (int64_t)(is_p ? np : gridDim.x - np) * 256;
   OutArgs o = a;
   o.mode = OUT_16;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+  for (int64_t i = (int64_t)(blockIdx.x - (is_p ? 0 : np)) * 256 + threadIdx.x; i < n; i += step) {
     const int64_t br = i / dc, b = br / a.R, r = br % a.R;
     const int d = (int)(i % dc) * 8;
     const float* p = a.f32 + (b * a.splits * a.R + r) * a.D + d;
@@ -1469,25 +1490,34 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
 }
 
 template <int DT>
-hipError_t launch_reduce(const OutArgs& q, int64_t nb, hipStream_t s) {
-  const int64_t n = nb * q.R * ((q.D + 7) / 8);
-  out_reduce_kernel<DT><<<dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 22)), 256, 0, s>>>(q, nb);
+hipError_t launch_reduce(const OutArgs& p, const OutArgs& q, int64_t nb, hipStream_t s) {
+  auto blocks = [&](const OutArgs& a) {
+    return a.mode == OUT_PART ? std::min<int64_t>((nb * a.R * ((a.D + 7) / 8) + 255) / 256, 1 << 20) : 0;
+  };
+  const int64_t np = blocks(p), nq = blocks(q);
+  if (np + nq == 0) return hipSuccess;
+  out_reduce_kernel<DT><<<dim3((unsigned)(np + nq)), 256, 0, s>>>(p, q, (int)np, nb);
   return hipGetLastError();
 }
 
+// Both products over nb instances: p's and q's contractions in `sp` and `sq` shares.
 template <int DT>
-hipError_t launch_out(OutArgs& q, int64_t nb, int splits, hipStream_t s) {
-  const bool narrow = q.D <= 128;
-  const int ba = narrow ? 128 : 256, nst = (q.chunks + 7) / 8;
-  q.per = (nst + splits - 1) / splits;
-  q.splits = (nst + q.per - 1) / q.per;
-  q.grid = make_raster((q.D + ba - 1) / ba, (q.R + LP_BB - 1) / LP_BB, nb * q.splits);
-  const dim3 grid((unsigned)q.grid.blocks());
-  if (narrow) out_kernel<DT, 1><<<grid, NT_T, 0, s>>>(q);
-  else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(q);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || q.mode != OUT_PART) return e;
-  return launch_reduce<DT>(q, nb, s);
+hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, hipStream_t s) {
+  const bool narrow = p.D <= 128;
+  auto plan = [&](OutArgs& a, int splits) {
+    const int nst = (a.chunks + 7) / 8;
+    a.per = (nst + splits - 1) / splits;
+    a.splits = (nst + a.per - 1) / a.per;
+    a.grid = make_raster((a.D + (narrow ? 127 : 255)) / (narrow ? 128 : 256),
+                         (a.R + LP_BB - 1) / LP_BB, nb * a.splits);
+    return a.grid.blocks();
+  };
+  const int64_t np = plan(p, sp), nq = plan(q, sq);
+  const dim3 grid((unsigned)(np + nq));
+  if (narrow) out_kernel<DT, 1><<<grid, NT_T, 0, s>>>(p, q, (int)np);
+  else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(p, q, (int)np);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_reduce<DT>(p, q, nb, s);
 }
 
 template <int DT>
@@ -1501,18 +1531,18 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     W = (const char*)w.wpad;
   }
   const int64_t lm = grad_ld(w.Mp);
-  // a wave has four rows of X and W or more, up to a workgroup per CU in all
-  const int64_t wgs = std::max<int64_t>(1, std::min<int64_t>(STATS_WGS, (a.M + a.V) / 32));
+  // blocks of about 64 KiB of rows, at most STATS_WGS / 2 workgroups for each of X and W
+  const int64_t rb = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / a.D));
+  const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
+  const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
   grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
       (const uint16_t*)a.X, (const uint16_t*)a.W, a.target, a.lse, a.entropy, a.g, a.h, a.bias, a.M,
-      (int)a.V, (int)a.D, w.rows, w.stats);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  grad_scales_kernel<<<dim3((unsigned)a.B), 64, 0, s>>>(w.stats, (int)wgs, w.scales);
+      (int)a.V, (int)a.D, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);
     const RowGrad* rg = w.rows + b0 * a.M;
-    const float4* scales = w.scales + b0;
+    float4* scales = w.scales + b0;
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
       const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
@@ -1521,7 +1551,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       const CopyJob jw{(const uint16_t*)a.W + b0 * a.V * a.D, a.V, v0, nv, vp, lv, nullptr, bias,
                        (uint16_t*)w.wt, (int)(vp / 64)};
       copy_kernel<DT><<<dim3((unsigned)(jx.tiles + jw.tiles), (unsigned)((a.D + 63) / 64), (unsigned)nb),
-                        256, 0, s>>>(jx, jw, (int)a.D, scales);
+                        256, 0, s>>>(jx, jw, (int)a.D, w.stats + b0 * wgs, (int)wgs, scales);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       DzArgs d;
       d.X = X + b0 * a.M * w.Dk * 2;
@@ -1556,23 +1586,23 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       if ((e = hipGetLastError()) != hipSuccess) return e;
 
       const bool whole = w.Vc >= a.V;  // one block of table rows
-      OutArgs q{};
-      q.D = (int)a.D;
+      OutArgs x{};
+      x.D = (int)a.D;
+      x.factor = a.scale / DZ_UP;
+      x.scales = scales;
+      OutArgs q = x;
       // dX: positions by D, over the table rows of this block
-      q.At = (const char*)w.wt;
-      q.Br = (const char*)w.dz;
-      q.ld = lv * 2;
-      q.as = a.D * q.ld;
-      q.bs = a.M * q.ld;
-      q.R = q.os = a.M;
-      q.chunks = (int)(vp / 8);
-      q.factor = a.scale / DZ_UP;
-      q.rows = rg;
-      q.scales = scales;
-      q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
-      q.mode = !whole ? (v0 ? OUT_ADD : OUT_FIRST) : w.sx > 1 ? OUT_PART : OUT_16;
-      q.f32 = whole ? w.part : w.accx;
-      if ((e = launch_out<DT>(q, nb, whole ? w.sx : 1, s)) != hipSuccess) return e;
+      x.At = (const char*)w.wt;
+      x.Br = (const char*)w.dz;
+      x.ld = lv * 2;
+      x.as = a.D * x.ld;
+      x.bs = a.M * x.ld;
+      x.R = x.os = a.M;
+      x.chunks = (int)(vp / 8);
+      x.rows = rg;
+      x.out = (uint16_t*)a.dX + b0 * a.M * a.D;
+      x.mode = !whole ? (v0 ? OUT_ADD : OUT_FIRST) : w.sx > 1 ? OUT_PART : OUT_16;
+      x.f32 = whole ? w.part : w.accx;
       // dW: the block's table rows by D, over the positions
       q.At = (const char*)w.xt;
       q.Br = (const char*)w.dzt;
@@ -1582,23 +1612,23 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.R = nv;
       q.os = a.V;
       q.chunks = (int)(w.Mp / 8);
-      q.rows = nullptr;
       q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
       q.mode = w.sw > 1 ? OUT_PART : OUT_16;
-      q.f32 = w.part;
-      if ((e = launch_out<DT>(q, nb, w.sw, s)) != hipSuccess) return e;
+      q.f32 = w.part + (x.mode == OUT_PART ? nb * w.sx * a.M * a.D : 0);
+      if ((e = launch_out<DT>(x, whole ? w.sx : 1, q, w.sw, nb, s)) != hipSuccess) return e;
     }
     if (w.Vc < a.V) {  // dX from its fp32 sums
-      OutArgs q{};
-      q.D = (int)a.D;
-      q.R = q.os = a.M;
-      q.splits = 1;
-      q.factor = a.scale / DZ_UP;
-      q.rows = rg;
-      q.scales = scales;
-      q.out = (uint16_t*)a.dX + b0 * a.M * a.D;
-      q.f32 = w.accx;
-      if ((e = launch_reduce<DT>(q, 1, s)) != hipSuccess) return e;
+      OutArgs x{}, none{};
+      x.D = (int)a.D;
+      x.R = x.os = a.M;
+      x.splits = 1;
+      x.mode = OUT_PART;
+      x.factor = a.scale / DZ_UP;
+      x.rows = rg;
+      x.scales = scales;
+      x.out = (uint16_t*)a.dX + b0 * a.M * a.D;
+      x.f32 = w.accx;
+      if ((e = launch_reduce<DT>(x, none, 1, s)) != hipSuccess) return e;
     }
   }
   return hipSuccess;

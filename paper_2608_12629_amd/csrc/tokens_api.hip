@@ -103,7 +103,7 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   take(w.rows, (size_t)(B * M) * sizeof(RowGrad));
-  take(w.stats, (size_t)(B * 256) * sizeof(float4));
+  take(w.stats, (size_t)(B * std::min(STATS_WGS, M + V)) * sizeof(float4));
   take(w.scales, (size_t)B * sizeof(float4));
   // sizes that never shrink as M grows, whatever the plan then is
   // (and 64 more elements a row: grad_ld)
@@ -117,7 +117,7 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
   const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);
   const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * D * (w.Mp / 512), cap);
-  take(w.part, (size_t)std::max(px, pw) * 4);
+  take(w.part, (size_t)(px + pw) * 4);
   w.total = take.o;
   return w;
 }

@@ -129,6 +129,7 @@ struct LogprobsArgs {
 // fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in fp16,
 // and both products read it and transposed fp16 copies of X and W.
 constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
+constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
 struct RowGrad {  // one position
   float g, h;     // gradients of the log probability and the entropy, over `gs`
   float lse, ent;
