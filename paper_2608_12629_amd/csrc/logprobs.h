@@ -500,7 +500,9 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
 
 // ---- few rows --------------------------------------------------------------------
 // Up to 64 rows (a decoding step): the table streams through once, bound by HBM.  A
-// workgroup owns 64 table rows and all positions; its four waves split the contraction
+// workgroup owns 64 table rows and up to 64 positions (more positions with a small table,
+// which then comes from L2 again, where tiles of 256 x 256 would leave the chip idle:
+// 256 x 5,000 x 1,024: FEW_US us); its four waves split the contraction
 // in units of 64 elements (whole 128-byte lines of each row), each wave holding 4 x CB
 // 16 x 16 x 32 MFMA tiles and loading the fragments of both operands straight into
 // registers, two units ahead, without LDS or barriers.  The waves' sums meet in LDS,
@@ -526,13 +528,13 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = blockIdx.y;
-  const int v0 = blockIdx.x * 64;
+  const int v0 = blockIdx.x * 64, m0 = blockIdx.z * (16 * CB);
   const char *pa[4], *pb[CB];
 #pragma unroll
   for (int i = 0; i < 4; ++i)
     pa[i] = a.W + (b * a.V + min(v0 + 16 * i + r16, a.V - 1)) * a.ld + q4 * 16;
 #pragma unroll
-  for (int i = 0; i < CB; ++i) pb[i] = a.X + (b * a.M + min(16 * i + r16, a.M - 1)) * a.ld + q4 * 16;
+  for (int i = 0; i < CB; ++i) pb[i] = a.X + (b * a.M + min(m0 + 16 * i + r16, a.M - 1)) * a.ld + q4 * 16;
   struct Unit {
     uint4 a[2][4], b[2][CB];
   };
@@ -595,30 +597,54 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
     for (int j = 0; j < CB; ++j)
       *reinterpret_cast<f32x4*>(&red[w][(16 * j + r16) * LDR + 16 * i + 4 * q4]) = acc[i][j];
   __syncthreads();
-  const int v = v0 + lane;
-  const float bz = BIAS && v < a.V ? a.bias[b * a.V + v] : 0.f;
-  const bool off = v >= a.V || (BIAS && bz == NEG_INF);
-  for (int m = w; m < a.M; m += 4) {
-    const int at = m * LDR + lane;
-    const float x = (red[0][at] + red[1][at]) + (red[2][at] + red[3][at]);
-    const float z = off ? NEG_INF : __builtin_fmaf(x, a.scale, bz);
-    float lm = z;
+  // 16 / CB lanes a position, 4 CB columns each
+  constexpr int TPM = 16 / CB, VPT = 4 * CB;
+  const int ml = tid / TPM, part = tid % TPM, m = m0 + ml;
+  const int vb = v0 + part * VPT;
+  float z[VPT], lm = NEG_INF;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) lm = __builtin_fmaxf(lm, __shfl_xor(lm, d));
-    const float mx = __builtin_fmaxf(lm, -__FLT_MAX__);
-    const float un = z - mx;
-    float s = __builtin_amdgcn_exp2f(un * LOG2E), t = s * __builtin_fmaxf(un, -1e30f);
+  for (int j = 0; j < VPT; j += 4) {
+    const int at = ml * LDR + part * VPT + j;
+    f32x4 x = (*reinterpret_cast<const f32x4*>(&red[0][at]) + *reinterpret_cast<const f32x4*>(&red[1][at])) +
+              (*reinterpret_cast<const f32x4*>(&red[2][at]) + *reinterpret_cast<const f32x4*>(&red[3][at]));
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      s += __shfl_xor(s, d);
-      t += __shfl_xor(t, d);
+    for (int r = 0; r < 4; ++r) {
+      const int v = vb + j + r;
+      const float bz = BIAS && v < a.V ? a.bias[b * a.V + v] : 0.f;
+      const bool off = v >= a.V || (BIAS && bz == NEG_INF);
+      z[j + r] = off ? NEG_INF : __builtin_fmaf(x[r], a.scale, bz);
+      lm = __builtin_fmaxf(lm, z[j + r]);
     }
-    if (lane == 0) a.part[(b * gridDim.x + blockIdx.x) * a.M + m] = make_float4(mx, s, t, 0.f);
-    if (a.target && v < a.V && a.target[b * a.M + m] == v) a.zt[b * a.M + m] = z;
-    if constexpr (TOPK) {
-      if (lane == 0) a.gmax[(b * a.M + m) * a.groups + blockIdx.x] = lm;
-      a.z[(b * a.M + m) * a.ldz + v] = z;
-    }
+  }
+#pragma unroll
+  for (int d = 1; d < TPM; d <<= 1) lm = __builtin_fmaxf(lm, __shfl_xor(lm, d));
+  const float mx = __builtin_fmaxf(lm, -__FLT_MAX__);
+  float s = 0.f, t = 0.f;
+#pragma unroll
+  for (int j = 0; j < VPT; ++j) {
+    const float un = z[j] - mx, e = __builtin_amdgcn_exp2f(un * LOG2E);
+    s += e;
+    t = __builtin_fmaf(e, __builtin_fmaxf(un, -1e30f), t);
+  }
+#pragma unroll
+  for (int d = 1; d < TPM; d <<= 1) {
+    s += __shfl_xor(s, d);
+    t += __shfl_xor(t, d);
+  }
+  if (m >= a.M) return;
+  if (part == 0) a.part[(b * gridDim.x + blockIdx.x) * a.M + m] = make_float4(mx, s, t, 0.f);
+  if (a.target) {
+    const int rel = a.target[b * a.M + m] - vb;
+#pragma unroll
+    for (int j = 0; j < VPT; ++j)
+      if (rel == j && vb + j < a.V) a.zt[b * a.M + m] = z[j];
+  }
+  if constexpr (TOPK) {
+    if (part == 0) a.gmax[(b * a.M + m) * a.groups + blockIdx.x] = lm;
+    float* zr = a.z + (b * a.M + m) * a.ldz + vb;
+#pragma unroll
+    for (int j = 0; j < VPT; j += 4)
+      *reinterpret_cast<f32x4*>(zr + j) = f32x4{z[j], z[j + 1], z[j + 2], z[j + 3]};
   }
 }
 
@@ -1378,7 +1404,7 @@ __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, i
 // ---- launchers -------------------------------------------------------------------
 template <int DT, int CB>
 hipError_t launch_few(const FewArgs& q, const LogprobsArgs& a, const LogprobsWs& w, hipStream_t s) {
-  const dim3 grid((unsigned)w.plan.splits, (unsigned)a.B);
+  const dim3 grid((unsigned)w.plan.splits, (unsigned)a.B, (unsigned)((a.M + 16 * CB - 1) / (16 * CB)));
   if (a.bias) {
     if (a.k) few_kernel<DT, CB, true, true><<<grid, 256, 0, s>>>(q);
     else few_kernel<DT, CB, true, false><<<grid, 256, 0, s>>>(q);

@@ -57,7 +57,7 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
   w.plan.rows = M;
   if (k) w.plan.rows = std::min(M, std::max<int64_t>(LP_SCORE_BYTES / (B * w.ldz * 4) / 256, 1) * 256);
   const int64_t nmb = cdiv(w.plan.rows, LP_BB), wgs = nmb * B;
-  w.plan.few = M <= LP_FEW_M;
+  w.plan.few = w.plan.rows == M && score_few(B, M, V, w.Dk);
   const int64_t nvb = w.ldz / 256, stages = cdiv(w.Dk, LP_DC);
   // A head of an eighth of the columns (of 8 groups for each of the k best at the least)
   // where storing every score would cost more than two launches: 4,096 x 65,536 x

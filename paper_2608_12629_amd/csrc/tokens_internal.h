@@ -92,10 +92,25 @@ inline int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
   }
   return best;
 }
-constexpr int64_t LP_FEW_M = 64;
+// Few rows, or few of both: workgroups of 64 columns by 64 rows, two to a CU, instead of
+// tiles.  Always up to 64 rows; else where the estimates, in us, say so: a workgroup's
+// fixed part and its quarter of the contraction in units of 64 elements, against a tile's
+// column blocks.
+constexpr int64_t LP_FEW_M = 64, LP_FEW_WGS = 2048;
+inline bool score_few(int64_t B, int64_t M, int64_t V, int64_t Dk) {
+  if (M <= LP_FEW_M) return true;
+  const int64_t units = (Dk + 63) / 64, wgs = (M + 63) / 64 * ((V + 63) / 64) * B;
+  if (wgs > LP_FEW_WGS) return false;
+  const int64_t nmb = (M + LP_BB - 1) / LP_BB, nvb = (V + 255) / 256;
+  const int s = score_splits(nmb, B, nvb, units);
+  const double few = (double)((wgs + 511) / 512) * (5 + 0.9 * (double)((units + 3) / 4));
+  const double tile = (double)((make_raster(s, nmb, B).blocks() + 255) / 256) *
+                      (3 + (double)((nvb + s - 1) / s) * (1.4 * (double)units + 4));
+  return few < tile;
+}
 struct LogprobsPlan {
   int64_t rows;    // rows of a block (all of M for k = 0)
-  bool few;        // up to LP_FEW_M rows: a workgroup for every 64 columns and all rows
+  bool few;        // a workgroup for every 64 columns and up to 64 rows
   // k > 0 and many scores: the first `head` column blocks in a launch of their own, whose
   // scores bound the k best from below; of the others only what exceeds that is stored
   int head, head_splits;
