@@ -720,9 +720,14 @@ __global__ __launch_bounds__(256) void finish_rows_kernel(FinishArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x, b = blockIdx.y;
   if (row >= a.rows) return;
   Stat st = stat_none();
-  for (int sp = 0; sp < a.splits; ++sp) {
-    const float4 p = a.part[(b * a.splits + sp) * a.rows + row];
-    st = stat_merge(st, Stat{p.x, p.y, p.z});
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {  // eight on their way at a time
+    float4 p[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      p[u] = a.part[(b * a.splits + min(s0 + u, a.splits - 1)) * a.rows + row];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (s0 + u < a.splits) st = stat_merge(st, Stat{p[u].x, p[u].y, p[u].z});
   }
   finish_row(a, b, row, st, logf(st.s));
 }
@@ -745,9 +750,14 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   __shared__ Stat sh[4];
   Stat st = stat_none();
-  for (int sp = tid; sp < a.splits; sp += 256) {
-    const float4 p = a.part[(b * a.splits + sp) * a.rows + row];
-    st = stat_merge(st, Stat{p.x, p.y, p.z});
+  for (int s0 = tid; s0 < a.splits; s0 += 4 * 256) {  // four on their way at a time
+    float4 p[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      p[u] = a.part[(b * a.splits + min(s0 + 256 * u, a.splits - 1)) * a.rows + row];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + 256 * u < a.splits) st = stat_merge(st, Stat{p[u].x, p[u].y, p[u].z});
   }
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) {
@@ -780,10 +790,16 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
     // with few groups (a table of up to 4,096 rows) the entries themselves
     const bool direct = G <= TOP_GROUPS;
     uint32_t mine = 0;
-    if (direct)
-      for (int i = tid; i < a.V; i += 256) mine = max(mine, score_key(zr[i]));
-    else
-      for (int i = tid; i < G; i += 256) mine = max(mine, score_key(gm[i]));
+    const float* src = direct ? zr : gm;
+    const int nsrc = direct ? a.V : G;
+    for (int i0 = tid; i0 < nsrc; i0 += 8 * 256) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = src[min(i0 + 256 * u, nsrc - 1)];  // the last one again
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (i0 + 256 * u < nsrc) mine = max(mine, score_key(x[u]));
+    }
     best[tid] = mine;
     if (tid == 0) ngroups = nentries = 0;
     __syncthreads();
@@ -796,27 +812,43 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
     }
     __syncthreads();
     const uint32_t bound = bound_s;
-    auto entry = [&](int v) {
-      const uint32_t key = score_key(zr[v]);
+    auto entry = [&](float z, int v) {
+      const uint32_t key = score_key(z);
       if (key >= bound) {
         const int at = atomicAdd(&nentries, 1);
         if (at < TOP_ENTRIES) ekey[at] = key, eidx[at] = v;
       }
     };
-    if (direct) {
-      for (int v = tid; v < a.V; v += 256) entry(v);
-    } else {
-      for (int i = tid; i < G; i += 256)
-        if (score_key(gm[i]) >= max(bound, nothing + 1)) {
+    for (int i0 = tid; i0 < nsrc; i0 += 8 * 256) {
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = src[min(i0 + 256 * u, nsrc - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int i = i0 + 256 * u;
+        if (i >= nsrc) continue;
+        if (direct) {
+          entry(x[u], i);
+        } else if (score_key(x[u]) >= max(bound, nothing + 1)) {
           const int at = atomicAdd(&ngroups, 1);
           if (at < TOP_GROUPS) sel[at] = i;
         }
+      }
+    }
+    if (!direct) {
       __syncthreads();
       const int ng = ngroups;
       if (ng > TOP_GROUPS) {
         if (tid == 0) nentries = TOP_ENTRIES + 1;
       } else {
-        for (int i = w; i < ng; i += 4) entry(sel[i] * LP_GROUP + lane);
+        for (int i0 = w; i0 < ng; i0 += 4 * 8) {
+          float x[8];
+#pragma unroll
+          for (int u = 0; u < 8; ++u) x[u] = zr[sel[min(i0 + 4 * u, ng - 1)] * LP_GROUP + lane];
+#pragma unroll
+          for (int u = 0; u < 8; ++u)
+            if (i0 + 4 * u < ng) entry(x[u], sel[i0 + 4 * u] * LP_GROUP + lane);
+        }
       }
     }
     __syncthreads();

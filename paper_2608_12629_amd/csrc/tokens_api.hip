@@ -151,11 +151,11 @@ int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, 
   if ((rc = check_ptrs({G, idx, dW}))) return rc;
   if ((rc = check_tokens(B, M, V, D, gdtype))) return rc;
   if (wdtype != gdtype && wdtype != DT_F32) return FKM_ERR_INVALID_ARG;
-  if (!ws || !aligned16(ws) || ws_bytes < embed_grad_carve(nullptr, B, M, V, D).total)
-    return FKM_ERR_WORKSPACE;
+  const EmbedGradWs w = embed_grad_carve(ws, B, M, V, D);
+  if (!ws || !aligned16(ws) || ws_bytes < w.total) return FKM_ERR_WORKSPACE;
   if ((rc = check_device())) return rc;
   return hip_status(launch_embed_grad(G, gdtype, idx, B, M, V, D, scale, accumulate != 0, dW, wdtype,
-                                      embed_grad_carve(ws, B, M, V, D), (hipStream_t)stream));
+                                      w, (hipStream_t)stream));
 }
 
 size_t tokens_logprobs_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int k,
@@ -175,12 +175,11 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
   if (k > 0 && (!top_idx || !top_logprob)) return FKM_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
   if ((rc = check_scores(B, M, V, D, k, xdtype))) return rc;
-  if (!ws || !aligned16(ws) || ws_bytes < logprobs_carve(nullptr, B, M, V, D, k).total)
-    return FKM_ERR_WORKSPACE;
+  const LogprobsWs w = logprobs_carve(ws, B, M, V, D, k);
+  if (!ws || !aligned16(ws) || ws_bytes < w.total) return FKM_ERR_WORKSPACE;
   if ((rc = check_device())) return rc;
   const LogprobsArgs a{X, W, bias, target, B, M, V, D, scale, k, logprob, entropy, lse, top_idx,
                        top_logprob};
-  const LogprobsWs w = logprobs_carve(ws, B, M, V, D, k);
   return hip_status((xdtype == DT_BF16 ? launch_logprobs_bf16 : launch_logprobs_f16)(
       a, w, (hipStream_t)stream));
 }
@@ -202,12 +201,11 @@ int tokens_logprobs_grad(const void* X, const void* W, int xdtype, const float* 
   if (grad_entropy && !entropy) return FKM_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
   if ((rc = check_scores(B, M, V, D, 0, xdtype))) return rc;
-  if (!ws || !aligned16(ws) || ws_bytes < grad_carve(nullptr, B, M, V, D).total)
-    return FKM_ERR_WORKSPACE;
+  const GradWs w = grad_carve(ws, B, M, V, D);
+  if (!ws || !aligned16(ws) || ws_bytes < w.total) return FKM_ERR_WORKSPACE;
   if ((rc = check_device())) return rc;
   const GradArgs a{X, W, bias, target, lse, entropy, grad_logprob, grad_entropy, B, M, V, D, scale,
                    dX, dW};
-  const GradWs w = grad_carve(ws, B, M, V, D);
   return hip_status((xdtype == DT_BF16 ? launch_logprobs_grad_bf16 : launch_logprobs_grad_f16)(
       a, w, (hipStream_t)stream));
 }

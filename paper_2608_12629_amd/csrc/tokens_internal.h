@@ -85,7 +85,7 @@ inline int score_splits(int64_t nmb, int64_t B, int64_t nvb, int64_t stages) {
   const int64_t most = std::min(nvb, std::max<int64_t>(1, SCORE_WGS / (nmb * B)));
   int best = 1;
   double least = HUGE_VAL;
-  for (int64_t s = 1; s <= most; s += s < 8 ? 1 : 8) {
+  for (int64_t s = 1; s <= most; s += s < 8 ? 1 : s < 64 ? 8 : s / 8 / 8 * 8) {
     const double us = (double)((make_raster(s, nmb, B).blocks() + 255) / 256) *
                       ((double)((nvb + s - 1) / s * stages) + 3);
     if (us < least) least = us, best = (int)s;

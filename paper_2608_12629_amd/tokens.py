@@ -12,7 +12,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from .kmeans import _DTYPE, ERR_UNSUPPORTED, KMeansError, _check, _need, _ptr, _stream, lib
+from .kmeans import _DTYPE, ERR_UNSUPPORTED, KMeansError, _check, _need, lib
 
 _i64, _i32, _vp, _sz, _f32 = (ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t,
                               ctypes.c_float)
@@ -33,6 +33,17 @@ for _f in (lib.tokens_embed_grad_workspace_bytes, lib.tokens_logprobs_workspace_
     _f.restype = ctypes.c_size_t
 
 
+# A call of a few microseconds should not wait for its own checks: the current device and
+# stream are asked for once, in the form that costs least.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _current() -> Tuple[int, Optional[int]]:
+    """The current device and its stream's handle."""
+    dev = torch.cuda.current_device()
+    return dev, _raw_stream(dev) if _raw_stream else torch.cuda.current_stream().cuda_stream
+
+
 def _dt(t: torch.Tensor, name: str) -> int:
     try:
         return _DTYPE[t.dtype]
@@ -40,30 +51,29 @@ def _dt(t: torch.Tensor, name: str) -> int:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}") from None
 
 
-def _rows(t: torch.Tensor, name: str) -> torch.Tensor:
+def _in(t: torch.Tensor, name: str, dev: int, dtype=None, numel: Optional[int] = None) -> int:
+    """The address of a tensor that passes kmeans._need's checks (which report what fails)."""
+    if (t.get_device() != dev or not t.is_contiguous() or (dtype is not None and t.dtype != dtype) or
+            (numel is not None and t.numel() != numel)):
+        _need(t, name, dtype, numel)
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     """[B, rows, D], or [rows, D] as one instance."""
-    if t.dim() not in (2, 3):
+    n = t.dim()
+    if n not in (2, 3):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, want [rows, D] or [B, rows, D]")
-    return t if t.dim() == 3 else t.unsqueeze(0)
+    return tuple(t.shape) if n == 3 else (1, *t.shape)
 
 
-def _out(t: Optional[torch.Tensor], name: str, shape: Tuple[int, ...], dtype, device) -> torch.Tensor:
-    if t is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    n = 1
-    for s in shape:
-        n *= s
-    _need(t, name, dtype, n)
-    return t
-
-
-def _workspace(ws: Optional[torch.Tensor], need: int, where: str, device) -> torch.Tensor:
+def _workspace(ws: Optional[torch.Tensor], need: int, where: str, like: torch.Tensor,
+               dev: int) -> Tuple[torch.Tensor, int]:
     if need == 0:
         raise KMeansError(ERR_UNSUPPORTED, where)
     if ws is None or ws.numel() < need:
-        ws = torch.empty(need, dtype=torch.uint8, device=device)
-    _need(ws, "ws", torch.uint8)
-    return ws
+        ws = torch.empty(need, dtype=torch.uint8, device=like.device)
+    return ws, _in(ws, "ws", dev, torch.uint8)
 
 
 def tokens_embed(table: torch.Tensor, idx: torch.Tensor, scale: float = 1.0,
@@ -71,16 +81,18 @@ def tokens_embed(table: torch.Tensor, idx: torch.Tensor, scale: float = 1.0,
     """scale * table[idx], ``[B, M, D]``; zero rows where there is no token (see
     ``tokens_embed`` in the header)."""
     dt = _dt(table, "table")
-    W = _rows(table, "table")
-    B, V, D = W.shape
-    _need(W, "table")
-    _need(idx, "idx", torch.int32)
-    M = idx.numel() // B if B else 0
-    if idx.dim() == 2 and idx.shape[0] != B or idx.dim() not in (1, 2) or M * B != idx.numel():
+    B, V, D = _rows(table, "table")
+    dev, stream = _current()
+    W = _in(table, "table", dev)
+    t = _in(idx, "idx", dev, torch.int32)
+    n = idx.dim()
+    if n not in (1, 2) or (idx.shape[0] if n == 2 else 1) != B:
         raise ValueError(f"idx has shape {tuple(idx.shape)}, want [B, M] with B = {B}")
-    out = _out(out, "out", (B, M, D), table.dtype, table.device)
-    _check(lib.tokens_embed(_ptr(W), dt, _ptr(idx), B, M, V, D, float(scale), _ptr(out), _stream()),
-           "tokens_embed")
+    M = idx.shape[-1]
+    if out is None:
+        out = torch.empty((B, M, D), dtype=table.dtype, device=table.device)
+    _check(lib.tokens_embed(W, dt, t, B, M, V, D, scale,
+                            _in(out, "out", dev, table.dtype, B * M * D), stream), "tokens_embed")
     return out
 
 
@@ -95,35 +107,34 @@ def tokens_embed_grad(grad: torch.Tensor, idx: torch.Tensor, V: int, scale: floa
     that of ``out`` (grad's or float32); ``accumulate`` adds it to what ``out`` holds
     (see ``tokens_embed_grad`` in the header)."""
     dt = _dt(grad, "grad")
-    G = _rows(grad, "grad")
-    B, M, D = G.shape
-    _need(G, "grad")
-    _need(idx, "idx", torch.int32, B * M)
-    if accumulate and out is None:
-        raise ValueError("accumulate adds to out: pass it in")
-    if out is not None and out.dtype not in (grad.dtype, torch.float32):
+    B, M, D = _rows(grad, "grad")
+    dev, stream = _current()
+    G = _in(grad, "grad", dev)
+    t = _in(idx, "idx", dev, torch.int32, B * M)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate adds to out: pass it in")
+        out = torch.empty((B, V, D), dtype=grad.dtype, device=grad.device)
+    elif out.dtype not in (grad.dtype, torch.float32):
         raise TypeError(f"out must be {grad.dtype} or float32, got {out.dtype}")
-    out = _out(out, "out", (B, V, D), grad.dtype if out is None else out.dtype, grad.device)
-    ws = _workspace(ws, embed_grad_workspace_bytes(B, M, V, D, grad.dtype), "tokens_embed_grad",
-                    grad.device)
-    _check(lib.tokens_embed_grad(_ptr(G), dt, _ptr(idx), B, M, V, D, float(scale), int(accumulate),
-                                 _ptr(out), _DTYPE[out.dtype], _ptr(ws), ws.numel(), _stream()),
-           "tokens_embed_grad")
+    o = _in(out, "out", dev, None, B * V * D)
+    ws, w = _workspace(ws, lib.tokens_embed_grad_workspace_bytes(B, M, V, D, dt), "tokens_embed_grad",
+                       grad, dev)
+    _check(lib.tokens_embed_grad(G, dt, t, B, M, V, D, scale, int(accumulate), o, _DTYPE[out.dtype], w,
+                                 ws.numel(), stream), "tokens_embed_grad")
     return out
 
 
-def _scored(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor]):
-    X, W = _rows(X, "X"), _rows(W, "W")
-    if X.shape[0] != W.shape[0] or X.shape[2] != W.shape[2]:
+def _scored(X: torch.Tensor, W: torch.Tensor, bias: Optional[torch.Tensor], dev: int):
+    B, M, D = _rows(X, "X")
+    Bw, V, Dw = _rows(W, "W")
+    if B != Bw or D != Dw:
         raise ValueError(f"shapes X{tuple(X.shape)} W{tuple(W.shape)}: want [B,M,D] and [B,V,D]")
     dt = _dt(X, "X")
     if X.dtype != W.dtype:
         raise TypeError("rows and table must share a dtype")
-    _need(X, "X")
-    _need(W, "W")
-    if bias is not None:
-        _need(bias, "bias", torch.float32, W.shape[0] * W.shape[1])
-    return X, W, dt
+    return (B, M, V, D, dt, _in(X, "X", dev), _in(W, "W", dev),
+            None if bias is None else _in(bias, "bias", dev, torch.float32, B * V))
 
 
 def logprobs_workspace_bytes(B: int, M: int, V: int, D: int, k: int, dtype: torch.dtype) -> int:
@@ -138,25 +149,36 @@ def tokens_logprobs(X: torch.Tensor, W: torch.Tensor, target: Optional[torch.Ten
     """(logprob, entropy, lse, top_idx, top_logprob) of the rows' softmax over the scores
     ``scale * X W^T + bias`` (see ``tokens_logprobs`` in the header).  logprob is None
     without a target, the last two with k = 0."""
-    X, W, dt = _scored(X, W, bias)
-    B, M, D = X.shape
-    V, dev, k = W.shape[1], X.device, int(k)
+    dev, stream = _current()
+    B, M, V, D, dt, x, w, bz = _scored(X, W, bias, dev)
+    k, f32, on = int(k), torch.float32, X.device
+    t = lp = ti = tl = None
     if target is not None:
-        _need(target, "target", torch.int32, B * M)
-        logprob = _out(logprob, "logprob", (B, M), torch.float32, dev)
+        t = _in(target, "target", dev, torch.int32, B * M)
+        if logprob is None:
+            logprob = torch.empty((B, M), dtype=f32, device=on)
+        lp = _in(logprob, "logprob", dev, f32, B * M)
     elif logprob is not None:
         raise ValueError("logprob needs a target")
-    entropy = _out(entropy, "entropy", (B, M), torch.float32, dev)
-    lse = _out(lse, "lse", (B, M), torch.float32, dev)
-    if k:
-        top_idx = _out(top_idx, "top_idx", (B, M, k), torch.int32, dev)
-        top_logprob = _out(top_logprob, "top_logprob", (B, M, k), torch.float32, dev)
+    if entropy is None:
+        entropy = torch.empty((B, M), dtype=f32, device=on)
+    if lse is None:
+        lse = torch.empty((B, M), dtype=f32, device=on)
+    if k > 0:
+        if top_idx is None:
+            top_idx = torch.empty((B, M, k), dtype=torch.int32, device=on)
+        if top_logprob is None:
+            top_logprob = torch.empty((B, M, k), dtype=f32, device=on)
+        ti = _in(top_idx, "top_idx", dev, torch.int32, B * M * k)
+        tl = _in(top_logprob, "top_logprob", dev, f32, B * M * k)
     elif top_idx is not None or top_logprob is not None:
         raise ValueError("top_idx and top_logprob need k > 0")
-    ws = _workspace(ws, logprobs_workspace_bytes(B, M, V, D, k, X.dtype), "tokens_logprobs", dev)
-    _check(lib.tokens_logprobs(_ptr(X), _ptr(W), dt, _ptr(bias), _ptr(target), B, M, V, D, float(scale),
-                               k, _ptr(logprob), _ptr(entropy), _ptr(lse), _ptr(top_idx),
-                               _ptr(top_logprob), _ptr(ws), ws.numel(), _stream()), "tokens_logprobs")
+    ws, p = _workspace(ws, lib.tokens_logprobs_workspace_bytes(B, M, V, D, k, dt), "tokens_logprobs", X,
+                       dev)
+    _check(lib.tokens_logprobs(x, w, dt, bz, t, B, M, V, D, scale, k, lp,
+                               _in(entropy, "entropy", dev, f32, B * M),
+                               _in(lse, "lse", dev, f32, B * M), ti, tl, p, ws.numel(), stream),
+           "tokens_logprobs")
     return logprob, entropy, lse, top_idx, top_logprob
 
 
@@ -171,24 +193,25 @@ def tokens_logprobs_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor,
                          dW: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
     """(dX, dW) of ``sum(grad_logprob * logprob + grad_entropy * entropy)``, from what
     ``tokens_logprobs`` returned (see ``tokens_logprobs_grad`` in the header)."""
-    X, W, dt = _scored(X, W, bias)
-    B, M, D = X.shape
-    V, dev = W.shape[1], X.device
-    _need(target, "target", torch.int32, B * M)
-    _need(lse, "lse", torch.float32, B * M)
-    _need(grad_logprob, "grad_logprob", torch.float32, B * M)
+    dev, stream = _current()
+    B, M, V, D, dt, x, w, bz = _scored(X, W, bias, dev)
+    f32, ent, h = torch.float32, None, None
+    t = _in(target, "target", dev, torch.int32, B * M)
+    l = _in(lse, "lse", dev, f32, B * M)
+    g = _in(grad_logprob, "grad_logprob", dev, f32, B * M)
     if grad_entropy is not None:
         if entropy is None:
             raise ValueError("grad_entropy needs the entropy of the forward pass")
-        _need(grad_entropy, "grad_entropy", torch.float32, B * M)
-        _need(entropy, "entropy", torch.float32, B * M)
-    else:
-        entropy = None
-    dX = _out(dX, "dX", (B, M, D), X.dtype, dev)
-    dW = _out(dW, "dW", (B, V, D), W.dtype, dev)
-    ws = _workspace(ws, logprobs_grad_workspace_bytes(B, M, V, D, X.dtype), "tokens_logprobs_grad", dev)
-    _check(lib.tokens_logprobs_grad(_ptr(X), _ptr(W), dt, _ptr(bias), _ptr(target), _ptr(lse),
-                                    _ptr(entropy), _ptr(grad_logprob), _ptr(grad_entropy), B, M, V, D,
-                                    float(scale), _ptr(dX), _ptr(dW), _ptr(ws), ws.numel(), _stream()),
+        h = _in(grad_entropy, "grad_entropy", dev, f32, B * M)
+        ent = _in(entropy, "entropy", dev, f32, B * M)
+    if dX is None:
+        dX = torch.empty((B, M, D), dtype=X.dtype, device=X.device)
+    if dW is None:
+        dW = torch.empty((B, V, D), dtype=X.dtype, device=X.device)
+    ws, p = _workspace(ws, lib.tokens_logprobs_grad_workspace_bytes(B, M, V, D, dt),
+                       "tokens_logprobs_grad", X, dev)
+    _check(lib.tokens_logprobs_grad(x, w, dt, bz, t, l, ent, g, h, B, M, V, D, scale,
+                                    _in(dX, "dX", dev, X.dtype, B * M * D),
+                                    _in(dW, "dW", dev, X.dtype, B * V * D), p, ws.numel(), stream),
            "tokens_logprobs_grad")
     return dX, dW
