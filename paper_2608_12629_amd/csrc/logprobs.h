@@ -1088,6 +1088,7 @@ struct CopyJob {
   const float* bias;    // of W
   uint16_t* out;
   int tiles;  // np / 64; 0: no such job
+  bool mixed; // columns 16 t + 8 h + i hold rows 16 t + 8 (i / 4) + 4 h + i % 4
 };
 template <int DT>
 __global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
@@ -1139,9 +1140,10 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
   for (int u = 0; u < 2; ++u) {
     const int r8 = t % 8, cl = t / 8 + 32 * u, c = ct + cl;
     const int64_t r = rt + 8 * r8;
-    const uint32_t* q = tile + cl * LD + 4 * r8;
+    const uint32_t* q = tile + cl * LD + (j.mixed ? 8 * (r8 >> 1) + 2 * (r8 & 1) : 4 * r8);
+    const int up = j.mixed ? 4 : 2;  // pairs to the second half
     if (c < C && r < j.np)
-      *reinterpret_cast<uint4*>(j.out + (b * C + c) * j.ldo + r) = make_uint4(q[0], q[1], q[2], q[3]);
+      *reinterpret_cast<uint4*>(j.out + (b * C + c) * j.ldo + r) = make_uint4(q[0], q[1], q[up], q[up + 1]);
   }
 }
 
@@ -1442,6 +1444,8 @@ __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, i
   }
 }
 
+#include "logprobs_narrow.h"
+
 // ---- launchers -------------------------------------------------------------------
 template <int DT, int CB, bool ONCE>
 hipError_t launch_few_once(const FewArgs& q, const LogprobsArgs& a, dim3 grid, hipStream_t s) {
@@ -1593,6 +1597,65 @@ hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, hipStr
   return e != hipSuccess ? e : launch_reduce<DT>(p, q, nb, s);
 }
 
+template <int DT, int DD>
+hipError_t launch_narrow_dd(const GradArgs& a, const NarrowArgs& x, const NarrowArgs& w,
+                            hipStream_t s) {
+  const int64_t nx = x.out.grid.blocks();
+  const dim3 grid((unsigned)(nx + w.out.grid.blocks()));
+  if (a.bias) {
+    if (a.h) narrow_kernel<DT, DD, true, true><<<grid, 256, 0, s>>>(x, w, (int)nx);
+    else narrow_kernel<DT, DD, true, false><<<grid, 256, 0, s>>>(x, w, (int)nx);
+  } else {
+    if (a.h) narrow_kernel<DT, DD, false, true><<<grid, 256, 0, s>>>(x, w, (int)nx);
+    else narrow_kernel<DT, DD, false, false><<<grid, 256, 0, s>>>(x, w, (int)nx);
+  }
+  return hipGetLastError();
+}
+template <int DT>
+hipError_t launch_narrow(const GradArgs& a, const GradWs& g, const char* X, const char* W,
+                         const float4* scales, int64_t lm, int64_t lv, hipStream_t s) {
+  NarrowArgs x{};
+  x.ld = g.Dk * 2;
+  x.chunks = (int)(g.Dk / 8);
+  x.V = (int)a.V;
+  x.M = a.M;
+  x.bias = a.bias;
+  x.rows = g.rows;
+  x.scale = a.scale;
+  x.out.D = (int)a.D;
+  x.out.factor = a.scale / DZ_UP;
+  x.out.scales = scales;
+  NarrowArgs w = x;
+  auto side = [&](NarrowArgs& n, const char* own, int64_t nown, const char* stream, int64_t nstream,
+                  const void* t, int64_t ldt, int splits, void* out, float* part) {
+    n.own = own;
+    n.stream = stream;
+    n.os = nown * n.ld;
+    n.ss = nstream * n.ld;
+    n.nown = (int)nown;
+    n.nstream = (int)nstream;
+    n.t = (const char*)t;
+    n.ldt = ldt * 2;
+    n.ts = a.D * n.ldt;
+    const int64_t stages = (nstream + 63) / 64;
+    n.per = (int)((stages + splits - 1) / splits);
+    n.out.splits = (int)((stages + n.per - 1) / n.per);
+    n.out.mode = n.out.splits > 1 ? OUT_PART : OUT_16;
+    n.out.R = n.out.os = nown;
+    n.out.out = (uint16_t*)out;
+    n.out.f32 = part;
+    n.out.grid = make_raster(n.out.splits, (nown + 127) / 128, a.B);
+  };
+  side(x, X, a.M, W, a.V, g.wt, lv, g.sx, a.dX, g.part);
+  x.out.rows = g.rows;
+  side(w, W, a.V, X, a.M, g.xt, lm, g.sw, a.dW,
+       g.part + (x.out.mode == OUT_PART ? a.B * g.sx * a.M * a.D : 0));
+  const hipError_t e = a.D <= 64 ? launch_narrow_dd<DT, 64>(a, x, w, s)
+                       : a.D <= 128 ? launch_narrow_dd<DT, 128>(a, x, w, s)
+                                    : launch_narrow_dd<DT, 256>(a, x, w, s);
+  return e != hipSuccess ? e : launch_reduce<DT>(x.out, w.out, a.B, s);
+}
+
 template <int DT>
 hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   hipError_t e;
@@ -1620,12 +1683,16 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
       const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
       const CopyJob jx{(const uint16_t*)a.X + b0 * a.M * a.D, a.M, 0, a.M, w.Mp, lm, rg, nullptr,
-                       (uint16_t*)w.xt, v0 ? 0 : (int)(w.Mp / 64)};
+                       (uint16_t*)w.xt, v0 ? 0 : (int)(w.Mp / 64), w.narrow};
       const CopyJob jw{(const uint16_t*)a.W + b0 * a.V * a.D, a.V, v0, nv, vp, lv, nullptr, bias,
-                       (uint16_t*)w.wt, (int)(vp / 64)};
+                       (uint16_t*)w.wt, (int)(vp / 64), w.narrow};
       copy_kernel<DT><<<dim3((unsigned)(jx.tiles + jw.tiles), (unsigned)((a.D + 63) / 64), (unsigned)nb),
                         256, 0, s>>>(jx, jw, (int)a.D, w.stats + b0 * wgs, (int)wgs, scales);
       if ((e = hipGetLastError()) != hipSuccess) return e;
+      if (w.narrow) {  // all instances and table rows at once
+        if ((e = launch_narrow<DT>(a, w, X, W, scales, lm, lv, s)) != hipSuccess) return e;
+        break;
+      }
       DzArgs d;
       d.X = X + b0 * a.M * w.Dk * 2;
       d.W = W + b0 * a.V * w.Dk * 2;

@@ -87,19 +87,32 @@ int out_splits(int64_t tiles, int64_t stages) {
   return (int)std::max<int64_t>(1, std::min(OUT_WGS / tiles, stages / 8));
 }
 
+// Shares of the streamed side over `blocks` workgroups: up to NARROW_WGS of a side in all
+// (both sides' two to a CU), of at least 4 stages.
+constexpr int64_t NARROW_WGS = 256;
+int narrow_splits(int64_t blocks, int64_t stages) {
+  return (int)std::max<int64_t>(1, std::min(NARROW_WGS / blocks, stages / 4));
+}
+
 GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   GradWs w{};
   Taker take{(char*)base};
   w.Dk = up(D, 8);
   w.Mp = up(M, 64);
   const int64_t Vall = up(V, 64), one = w.Mp * Vall * 4;
-  w.nb = B * one <= LP_DZ_BYTES ? (int)B : 1;
-  w.Vc = w.nb * one <= LP_DZ_BYTES || V <= 256
+  w.narrow = D <= LP_NARROW;
+  w.nb = w.narrow || B * one <= LP_DZ_BYTES ? (int)B : 1;
+  w.Vc = w.narrow || w.nb * one <= LP_DZ_BYTES || V <= 256
              ? V : std::min(V, std::max<int64_t>(LP_DZ_BYTES / (4 * w.Mp) / 256, 1) * 256);
   w.Vp = up(w.Vc, 64);
-  const int64_t ba = D <= 128 ? 128 : 256, dt = cdiv(D, ba);
-  w.sx = out_splits(w.nb * cdiv(M, LP_BB) * dt, w.Vp / LP_DC);
-  w.sw = out_splits(w.nb * cdiv(w.Vc, LP_BB) * dt, w.Mp / LP_DC);
+  const int64_t dt = cdiv(D, 256);
+  if (w.narrow) {
+    w.sx = narrow_splits(B * cdiv(M, 128), Vall / 64);
+    w.sw = narrow_splits(B * cdiv(V, 128), w.Mp / 64);
+  } else {
+    w.sx = out_splits(w.nb * cdiv(M, LP_BB) * dt, w.Vp / LP_DC);
+    w.sw = out_splits(w.nb * cdiv(w.Vc, LP_BB) * dt, w.Mp / LP_DC);
+  }
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
   take(w.rows, (size_t)(B * M) * sizeof(RowGrad));
@@ -109,15 +122,19 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   // (and 64 more elements a row: grad_ld)
   const size_t dz = (size_t)(std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2) +
                              B * std::max(w.Mp, Vall) * 64 * 2);
-  take(w.dz, dz);
-  take(w.dzt, dz);
+  take(w.dz, w.narrow ? 0 : dz);
+  take(w.dzt, w.narrow ? 0 : dz);
   take(w.xt, (size_t)(B * D * (w.Mp + 64)) * 2);
   take(w.wt, (size_t)(B * D * (Vall + 64)) * 2);
   take(w.accx, w.Vc < V ? (size_t)(M * D) * 4 : 0);
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
   const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);
   const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * D * (w.Mp / 512), cap);
-  take(w.part, (size_t)(px + pw) * 4);
+  // narrow: at most NARROW_WGS x 128 rows of a side in shares
+  const double ncap = (double)NARROW_WGS * 128 * (double)D;
+  const double nx = std::min((double)B * M * D * std::max<int64_t>(1, Vall / 256), ncap);
+  const double nw = std::min((double)B * V * D * std::max<int64_t>(1, w.Mp / 256), ncap);
+  take(w.part, (size_t)(w.narrow ? nx + nw : px + pw) * 4);
   w.total = take.o;
   return w;
 }
