@@ -996,13 +996,13 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
           int e;
           (void)frexpf(big, &e);
           e = min(max(e, -120), 120);
-          r.gs = ldexpf(1.f, e);
-          r.g *= ldexpf(1.f, -e);
-          r.h *= ldexpf(1.f, -e);
+          r.gs = copysignf(ldexpf(1.f, e), r.g);
+          r.g *= copysignf(ldexpf(1.f, -e), r.g);
+          r.h *= 1.f / r.gs;
         }
         out[i] = r;
         part[tid] = r.active;
-        if (r.active) gsmax = __builtin_fmaxf(gsmax, r.gs);
+        if (r.active) gsmax = __builtin_fmaxf(gsmax, __builtin_fabsf(r.gs));
       } else {
         part[tid] = !bias || bias[b * V + r0 + tid] != NEG_INF;
       }
@@ -1303,7 +1303,7 @@ struct OutArgs {
   int64_t ld;          // bytes of a row of either
   int64_t R, os;       // rows, rows between instances of the output
   int D, chunks, per;  // chunks of the contraction, stages of a share
-  int splits, mode;
+  int splits, mode, lanes;
   float factor;
   const RowGrad* rows;   // dX: times gs of the row, over W's factor
   const float4* scales;  // dW (rows NULL): times the largest gs, over X's factor
@@ -1411,37 +1411,41 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int 
   loop.template run<false>(epi);
 }
 
-// out[b, r, d] = the sum over the shares of part[b, s, r, d] in their order, times its
-// factor; eight results a thread.
+// out[b, r, d] = the sum over the shares of part[b, s, r, d], times its factor: eight
+// results by `lanes` threads, each with every lanes-th share in order, then a tree.
 template <int DT>
 __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, int np, int64_t nb) {
   const bool is_p = (int)blockIdx.x < np;
   const OutArgs a = is_p ? p : q;
-  const int dc = (a.D + 7) / 8;
-  const int64_t n = nb * a.R * dc, step = (int64_t)(is_p ? np : gridDim.x - np) * 256;
+  const int dc = (a.D + 7) / 8, l = threadIdx.x % a.lanes, per = 256 / a.lanes;
+  const int64_t n = nb * a.R * dc;
+  const int64_t i = (int64_t)(blockIdx.x - (is_p ? 0 : np)) * per + threadIdx.x / a.lanes;
   OutArgs o = a;
   o.mode = OUT_16;
-  for (int64_t i = (int64_t)(blockIdx.x - (is_p ? 0 : np)) * 256 + threadIdx.x; i < n; i += step) {
-    const int64_t br = i / dc, b = br / a.R, r = br % a.R;
-    const int d = (int)(i % dc) * 8;
-    const float* p = a.f32 + (b * a.splits * a.R + r) * a.D + d;
-    float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-    for (int s = 0; s < a.splits; ++s, p += a.R * a.D) {
-      if (a.D % 8 == 0) {
+  const int64_t br = min(i, n - 1) / dc, b = br / a.R, r = br % a.R;
+  const int d = (int)(min(i, n - 1) % dc) * 8;
+  const float* from = a.f32 + (b * a.splits * a.R + r) * a.D + d;
+  float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  for (int s = l; s < a.splits; s += a.lanes) {
+    const float* x = from + s * (a.R * a.D);
+    if (a.D % 8 == 0) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 4) {
-          const f32x4 x = *reinterpret_cast<const f32x4*>(p + e);
+      for (int e = 0; e < 8; e += 4) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(x + e);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[e + k] += x[k];
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (d + e < a.D) v[e] += p[e];
+        for (int k = 0; k < 4; ++k) v[e + k] += y[k];
       }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (d + e < a.D) v[e] += x[e];
     }
-    out_store<DT>(o, b, 0, r, d, v);
   }
+  for (int m = 1; m < a.lanes; m <<= 1) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], m);
+  }
+  if (l == 0 && i < n) out_store<DT>(o, b, 0, r, d, v);
 }
 
 #include "logprobs_narrow.h"
@@ -1567,9 +1571,16 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
 }
 
 template <int DT>
-hipError_t launch_reduce(const OutArgs& p, const OutArgs& q, int64_t nb, hipStream_t s) {
-  auto blocks = [&](const OutArgs& a) {
-    return a.mode == OUT_PART ? std::min<int64_t>((nb * a.R * ((a.D + 7) / 8) + 255) / 256, 1 << 20) : 0;
+hipError_t launch_reduce(OutArgs& p, OutArgs& q, int64_t nb, hipStream_t s) {
+  // more threads to a result while there are few results: many shares of few rows would
+  // be as many latencies one after another (one position, 131,072 x 1,024:
+  // the call 519 -> 460 us)
+  auto blocks = [&](OutArgs& a) -> int64_t {
+    if (a.mode != OUT_PART) return 0;
+    const int64_t n = nb * a.R * ((a.D + 7) / 8);
+    a.lanes = 1;
+    while (a.lanes < 64 && a.lanes * 4 <= a.splits && n * a.lanes < 65536) a.lanes *= 2;
+    return (n * a.lanes + 255) / 256;
   };
   const int64_t np = blocks(p), nq = blocks(q);
   if (np + nq == 0) return hipSuccess;
@@ -1623,7 +1634,7 @@ hipError_t launch_narrow(const GradArgs& a, const GradWs& g, const char* X, cons
   x.rows = g.rows;
   x.scale = a.scale;
   x.out.D = (int)a.D;
-  x.out.factor = a.scale / DZ_UP;
+  x.out.factor = (a.h ? a.scale : -a.scale) / DZ_UP;  // (see dz_of)
   x.out.scales = scales;
   NarrowArgs w = x;
   auto side = [&](NarrowArgs& n, const char* own, int64_t nown, const char* stream, int64_t nstream,

@@ -87,11 +87,11 @@ int out_splits(int64_t tiles, int64_t stages) {
   return (int)std::max<int64_t>(1, std::min(OUT_WGS / tiles, stages / 8));
 }
 
-// Shares of the streamed side over `blocks` workgroups: up to NARROW_WGS of a side in all
-// (both sides' two to a CU), of at least 4 stages.
-constexpr int64_t NARROW_WGS = 256;
-int narrow_splits(int64_t blocks, int64_t stages) {
-  return (int)std::max<int64_t>(1, std::min(NARROW_WGS / blocks, stages / 4));
+// Shares of the streamed side over `blocks` workgroups: up to narrow_wgs of a side in all
+// (both sides' fill the CUs once), of at least 4 stages.
+int64_t narrow_wgs(int64_t D) { return D <= 64 ? 512 : 256; }
+int narrow_splits(int64_t blocks, int64_t stages, int64_t D) {
+  return (int)std::max<int64_t>(1, std::min(narrow_wgs(D) / blocks, stages / 4));
 }
 
 GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
@@ -100,15 +100,22 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   w.Dk = up(D, 8);
   w.Mp = up(M, 64);
   const int64_t Vall = up(V, 64), one = w.Mp * Vall * 4;
-  w.narrow = D <= LP_NARROW;
+  // dz is not stored for rows of up to 128 elements (us, stored / not, 64 x 64 x 64 23 /
+  // 16, 10,007 x 1,003 x 128 52 / 46, 16,384 x 4,096 x 128 240 / 104).  From there to 256
+  // the four products take longer than storing as long as dz stays in the caches: not
+  // stored where the calls are short or the two copies of dz (4 bytes a score) pass 128
+  // MiB (1,000 x 1,000 x 256 48 / 38, 10,007 x 1,003 x 200 65 / 74, 4,096 x 4,096 x 256
+  // 79 / 87, 8,192 x 8,192 x 256 328 / 202).
+  const int64_t scores = B * w.Mp * Vall;
+  w.narrow = D <= 128 || (D <= LP_NARROW && (scores <= 1 << 22 || scores >= LP_NARROW_SCORES));
   w.nb = w.narrow || B * one <= LP_DZ_BYTES ? (int)B : 1;
   w.Vc = w.narrow || w.nb * one <= LP_DZ_BYTES || V <= 256
              ? V : std::min(V, std::max<int64_t>(LP_DZ_BYTES / (4 * w.Mp) / 256, 1) * 256);
   w.Vp = up(w.Vc, 64);
   const int64_t dt = cdiv(D, 256);
   if (w.narrow) {
-    w.sx = narrow_splits(B * cdiv(M, 128), Vall / 64);
-    w.sw = narrow_splits(B * cdiv(V, 128), w.Mp / 64);
+    w.sx = narrow_splits(B * cdiv(M, 128), Vall / 64, D);
+    w.sw = narrow_splits(B * cdiv(V, 128), w.Mp / 64, D);
   } else {
     w.sx = out_splits(w.nb * cdiv(M, LP_BB) * dt, w.Vp / LP_DC);
     w.sw = out_splits(w.nb * cdiv(w.Vc, LP_BB) * dt, w.Mp / LP_DC);
@@ -122,19 +129,21 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   // (and 64 more elements a row: grad_ld)
   const size_t dz = (size_t)(std::max(std::min(B * one, LP_DZ_BYTES) / 2, w.Mp * 256 * 2) +
                              B * std::max(w.Mp, Vall) * 64 * 2);
-  take(w.dz, w.narrow ? 0 : dz);
-  take(w.dzt, w.narrow ? 0 : dz);
+  const size_t held = D <= 128 ? 0 : D > LP_NARROW ? dz :
+      (size_t)(std::min(scores, LP_NARROW_SCORES) + B * std::max(w.Mp, Vall) * 64) * 2;
+  take(w.dz, held);
+  take(w.dzt, held);
   take(w.xt, (size_t)(B * D * (w.Mp + 64)) * 2);
   take(w.wt, (size_t)(B * D * (Vall + 64)) * 2);
   take(w.accx, w.Vc < V ? (size_t)(M * D) * 4 : 0);
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
   const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);
   const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * D * (w.Mp / 512), cap);
-  // narrow: at most NARROW_WGS x 128 rows of a side in shares
-  const double ncap = (double)NARROW_WGS * 128 * (double)D;
+  // narrow: at most narrow_wgs x 128 rows of a side in shares
+  const double ncap = (double)narrow_wgs(D) * 128 * (double)D;
   const double nx = std::min((double)B * M * D * std::max<int64_t>(1, Vall / 256), ncap);
   const double nw = std::min((double)B * V * D * std::max<int64_t>(1, w.Mp / 256), ncap);
-  take(w.part, (size_t)(w.narrow ? nx + nw : px + pw) * 4);
+  take(w.part, (size_t)(D <= 128 ? nx + nw : D <= LP_NARROW ? std::max(nx + nw, px + pw) : px + pw) * 4);
   w.total = take.o;
   return w;
 }

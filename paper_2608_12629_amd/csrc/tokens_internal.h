@@ -144,14 +144,14 @@ struct LogprobsArgs {
 // fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in fp16,
 // and both products read it and transposed fp16 copies of X and W.
 constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
-constexpr int64_t LP_NARROW = 256;
+constexpr int64_t LP_NARROW = 256, LP_NARROW_SCORES = 1 << 25;
 constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
 struct RowGrad {  // one position
-  float g, h;     // gradients of the log probability and the entropy, over `gs`
+  float g, h;     // gradients of the log probability (>= 0) and the entropy, over `gs`
   float lse, ent;
   int target;     // -1: none
   int active;     // takes part at all
-  float gs;       // a power of two: what g, h and so dz of this row are divided by
+  float gs;       // a power of two with g's sign: what g, h and so dz of this row are divided by
   int pad;
 };
 // Elements from row to row of dz and the copies: 128 bytes past a multiple of 1 KiB, so
@@ -167,7 +167,7 @@ struct GradWs {
   float* accx;      // [M, D] dX over the blocks of table rows, where there are several
   float* part;      // [nb, splits, rows, D] shares of a contraction
   int64_t Dk, Mp, Vp, Vc;
-  bool narrow;      // rows of up to LP_NARROW: dz is not stored (logprobs_narrow.h)
+  bool narrow;      // short rows: dz is not stored (logprobs_narrow.h)
   int nb;           // instances at a time (B or 1)
   int sx, sw;       // shares of dX's and dW's contractions
   size_t total;
