@@ -14,7 +14,9 @@
  * - A position whose token lies outside [0, V) (kmeans_assign's -1, padding) has
  *   no token: a zero row, log probability 0, no gradient.
  * - Offsets are 64 bits wide: no array has a size limit of its own.  B up to
- *   65,535, M up to 2^24, V up to 2^20, D up to 8,192.
+ *   65,535, M up to 2^24 (2^23 - 64 for tokens_logprobs_grad), V up to 2^20, D up
+ *   to 8,192.
+ * - Outputs overlap neither inputs, nor each other, nor the workspace.
  */
 #ifndef FLASHTOKENS_H_
 #define FLASHTOKENS_H_
@@ -79,8 +81,9 @@ int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, 
  * with k = 0 the last two are not used.  A row all of whose tokens are forbidden
  * has lse and logprob -inf and entropy 0.  xdtype bf16 or fp16 (fp32 is
  * FKM_ERR_UNSUPPORTED).  A row of X with a NaN has NaN results and no other
- * row has; its top_idx are valid or -1.  D that is no multiple of 8 runs on padded copies.  scale
- * must be finite.  Scores that overflow fp32 are outside the contract.
+ * row has; its top_idx are valid or -1.  D that is no multiple of 8 runs on padded
+ * copies.  scale must be finite.  Scores that overflow fp32 are outside the
+ * contract.
  * Workspace: tokens_logprobs_workspace_bytes.
  */
 size_t tokens_logprobs_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int k,
@@ -104,8 +107,9 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
  * A position without a token, or whose token is forbidden, has no gradient of
  * its log probability; a row with neither gradient, or with lse -inf, is not
  * used at all (it may hold anything) and gets dX 0.  Forbidden tokens get dW 0.
- * dz is rounded to 16 bits (as X and W are) before the two products, each of
- * which sums in fp32 in a fixed order and rounds once.
+ * The two products take dz, X and W in fp16, each brought to fp16's range by powers
+ * of two (dz over each position's own, X and W over their largest value's), sum in
+ * fp32 in a fixed order and round once.
  * Workspace: tokens_logprobs_grad_workspace_bytes.
  */
 size_t tokens_logprobs_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int xdtype);

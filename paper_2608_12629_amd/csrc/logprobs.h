@@ -502,12 +502,12 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
 // Up to 64 rows (a decoding step): the table streams through once, bound by HBM.  A
 // workgroup owns 64 table rows and up to 64 positions (more positions with a small table,
 // which then comes from L2 again, where tiles of 256 x 256 would leave the chip idle:
-// 256 x 5,000 x 1,024: FEW_US us); its four waves split the contraction
+// 256 x 5,000 x 1,024: 52 -> 24 us); its four waves split the contraction
 // in units of 64 elements (whole 128-byte lines of each row), each wave holding 4 x CB
 // 16 x 16 x 32 MFMA tiles and loading the fragments of both operands straight into
 // registers, two units ahead, without LDS or barriers.  The waves' sums meet in LDS,
 // where each wave then has the 64 scores of a position in its lanes.  131,072 x 4,096
-// bf16: one row 264 -> 186 us (5.8 TB/s), against the tiles of 256 positions.
+// bf16: one row 264 -> 187 us (5.7 TB/s), against the tiles of 256 positions.
 struct FewArgs {
   const char *X, *W;
   const float* bias;

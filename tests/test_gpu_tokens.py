@@ -475,3 +475,203 @@ def test_the_binding_refuses(tk):
     with pytest.raises(ValueError, match="dW has"):
         tk.tokens_logprobs_grad(X, W, t, lse, g, dW=torch.empty((2, 29, 64), dtype=BF, device="cuda"))
     torch.cuda.synchronize()
+
+
+# ---- sizes and masks at which the kernels' paths part -----------------------------------
+@pytest.mark.parametrize("B,M,V,D,dt", [(1, 200, 40, 64, BF), (1, 256, 300, 1000, F16), (8, 100, 60, 72, BF),
+                                        (2, 1000, 33, 16, BF), (1, 65, 64, 8, F16), (5, 4096, 31, 128, BF)])
+def test_many_rows_of_small_tables(tk, B, M, V, D, dt):
+    X, W, t = grid_rows((B, M, D), dt, 131), grid_rows((B, V, D), dt, 132), ids(B, M, V, 133)
+    W[:, V // 2:V // 2 * 2] = W[:, :V // 2].clone()
+    for k in (0, min(V, 7)):
+        check_logprobs(tk, X, W, t, 0.125, None, k, f"{B, M, V, D, dt} k={k}")
+    bias = torch.where(rows((B, V), F32, 134) > 0.5, -INF, rows((B, V), F32, 135).round())
+    check_logprobs(tk, X, W, t, -0.25, bias, min(V, 32), "masked")
+
+
+@pytest.mark.parametrize("k", [1, 20, 32])
+def test_alternatives_outside_a_head(tk, k):
+    """Many scores: the best ones of the first columns bound the rest.  Those first ones
+    forbidden, fewer than k left anywhere, all forbidden, all equal, and every one twice."""
+    M, V, D = 300, 70_000, 32
+    X, W, t = grid_rows((1, M, D), BF, 141), grid_rows((1, V, D), BF, 142), ids(1, M, V, 143)
+    W[:, V // 2:] = W[:, :V // 2].clone()
+    check_logprobs(tk, X, W, t, 0.25, None, k, "twice")
+    bias = torch.zeros((1, V), device="cuda")
+    bias[:, :V // 2] = -INF
+    check_logprobs(tk, X, W, t, 0.25, bias, k, "first half forbidden")
+    bias[:, 5::3] = -INF
+    bias[:, V - 300:] = 2.0
+    check_logprobs(tk, X, W, t, -0.25, bias, k, "best last")
+    bias.fill_(-INF)
+    bias[0, torch.tensor([3, 40_000, 69_999], device="cuda")] = torch.tensor([1.0, 0.0, 1.0], device="cuda")
+    got = check_logprobs(tk, X, W, t, 0.25, bias, k, "three left")
+    assert (got[3][..., 3:] == -1).all()
+    bias.fill_(-INF)
+    got = check_logprobs(tk, X, W, t, 0.25, bias, k, "none left")
+    assert (got[3] == -1).all()
+    got = check_logprobs(tk, X, W, t, 0.0, None, k, "all equal")
+    assert torch.equal(got[3], torch.arange(k, device="cuda", dtype=torch.int32).expand(1, M, k))
+
+
+def test_alternatives_with_nan_rows_of_many_scores(tk):
+    M, V, D = 300, 60_000, 24
+    X, W, t = grid_rows((1, M, D), F16, 145), grid_rows((1, V, D), F16, 146), ids(1, M, V, 147)
+    clean = [a.clone() for a in tk.tokens_logprobs(X, W, t, k=6, scale=0.25)]
+    bad = [0, 131, 255, 256, 299]
+    X[0, bad, 5] = float("nan")
+    got = tk.tokens_logprobs(X, W, t, k=6, scale=0.25)
+    keep = torch.ones(M, dtype=torch.bool, device="cuda")
+    keep[bad] = False
+    for a, b in zip(clean, got):
+        assert torch.equal(a[0, keep], b[0, keep])
+    assert got[2][0, bad].isnan().all() and (got[3] < V).all() and (got[3] >= -1).all()
+
+
+NARROW = [(1, 63, 65, 1, BF), (1, 64, 64, 16, F16), (2, 65, 129, 64, BF), (1, 129, 127, 65, F16),
+          (3, 128, 1, 128, BF), (1, 1, 128, 128, F16), (1, 130, 600, 129, BF), (1, 2_000, 500, 136, F16),
+          (2, 300, 300, 192, BF), (1, 900, 4_100, 256, BF), (1, 2_100, 2_100, 256, F16),
+          (1, 6_000, 5_700, 256, BF), (1, 4_100, 8_300, 130, BF), (2, 9_000, 2_000, 224, F16),
+          (3, 1_030, 900, 31, F16), (1, 20_000, 1_100, 48, BF)]
+
+
+@pytest.mark.parametrize("B,M,V,D,dt", NARROW)
+def test_gradients_of_short_rows(tk, B, M, V, D, dt):
+    X, W, t = rows((B, M, D), dt, 151), rows((B, V, D), dt, 152), ids(B, M, V, 153)
+    g, h = rows((B, M), F32, 154), rows((B, M), F32, 155, 0.3)
+    bias = rows((B, V), F32, 156)
+    bias[rows((B, V), F32, 157) > 0.9] = -INF
+    scale = 1.7 / D ** 0.5
+    g[:, ::5] = 0
+    for b, e in ((None, None), (bias, None), (None, h), (bias, h)):
+        check_grads(tk, X, W, t, g, e, scale, b, f"{B, M, V, D, dt} {b is not None} {e is not None}")
+
+
+def test_gradients_of_short_rows_that_take_no_part(tk):
+    """Idle positions with NaN, forbidden tokens with NaN, and the last of either idle."""
+    for M, V, D in ((193, 257, 40), (700, 129, 200), (70, 1_000, 128)):
+        X, W, t = rows((1, M, D), BF, 161), rows((1, V, D), BF, 162), ids(1, M, V, 163)
+        for h in (None, rows((1, M), F32, 165, 0.1)):
+            g = rows((1, M), F32, 164)
+            idle = torch.arange(M, device="cuda") % 3 == (M - 1) % 3
+            g[:, idle] = 0
+            if h is not None:
+                h[:, idle] = 0
+            bias = torch.zeros((1, V), device="cuda")
+            bias[:, (V - 1) % 5::5] = -INF
+            for b in (None, bias):
+                want = check_grads(tk, X, W, t, g, h, 0.2, b, f"{M, V, D} idle")
+                _, ent, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.2, bias=b)
+                X2, W2, lse2 = X.clone(), W.clone(), lse.clone()
+                X2[:, idle] = float("nan")
+                lse2[:, idle] = float("nan")
+                if b is not None:
+                    W2[:, (V - 1) % 5::5] = float("nan")
+                got = tk.tokens_logprobs_grad(X2, W2, t, lse2, g, entropy=ent if h is not None else None,
+                                              grad_entropy=h, scale=0.2, bias=b)
+                assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_gradients_with_scale_zero_and_sharp_rows(tk):
+    X, W, t = rows((1, 150, 64), F16, 171), rows((1, 300, 64), F16, 172), ids(1, 150, 300, 173)
+    g = rows((1, 150), F32, 174)
+    dX, dW = check_grads(tk, X, W, t, g, None, 0.0, None, "scale 0")
+    assert not dX.any() and not dW.any()
+    # one token has all the probability: p is 1 or 0
+    check_grads(tk, X, W, t, g, rows((1, 150), F32, 175, 0.1), 30.0, None, "sharp")
+    bias = torch.full((1, 300), LOWEST, device="cuda")
+    bias[:, 7] = 0
+    check_grads(tk, X, W, t, g, rows((1, 150), F32, 176, 0.1), 0.3, bias, "the lowest value")
+
+
+@pytest.mark.parametrize("B,M,V,D", [(1, 6_000, 50_000, 264), (2, 3_000, 50_000, 260)])
+def test_blocks_of_table_rows_of_long_rows(tk, B, M, V, D):
+    X, W, t = rows((B, M, D), BF, 181), rows((B, V, D), BF, 182), ids(B, M, V, 183)
+    check_grads(tk, X, W, t, rows((B, M), F32, 184), None, 0.1, None, f"{B, M, V, D}")
+
+
+@pytest.mark.parametrize("M,V,D", [(5_000_000, 40, 264), (6_000_001, 70, 250)])
+def test_gradients_of_millions_of_positions(tk, M, V, D):
+    """Offsets past 2^31 bytes within a block of rows; the reference in parts."""
+    X, W, t = rows((1, M, D), BF, 191), rows((1, V, D), BF, 192), ids(1, M, V, 193)
+    g = rows((1, M), F32, 194)
+    _, _, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.1)
+    dX, dW = tk.tokens_logprobs_grad(X, W, t, lse, g, scale=0.1)
+    total, err = 0, 0
+    part = 500_000
+    for m in range(0, M, part):
+        s = slice(m, min(M, m + part))
+        wX, wW, eX, eW = ref.grads(X[:, s], W, t[:, s], g[:, s], None, 0.1)
+        bad = ((dX[:, s].double() - wX).abs() > eX)
+        assert not bad.any(), (m, int(bad.sum()))
+        total, err = total + wW, err + eW
+    # (the parts' bounds together hold for their sum; a running sum of M terms in fp32
+    # within the shares is what eW counts as X.shape[1] steps of a part: M / part times it)
+    within(dW, total, err * (M / part), "dW")
+
+
+def test_embed_grad_by_radix_in_instances(tk):
+    for B, M, V, D in ((3, 5_000, 77, 16), (2, 8_193, 70_000, 8), (9, 8_192, 5, 33)):
+        G, t = rows((B, M, D), BF, 201), ids(B, M, V, 202)
+        want, bound = ref.embed_grad(G, t, V, 0.7)
+        got = tk.tokens_embed_grad(G, t, V, 0.7)
+        within(got, want, bound, f"{B, M, V, D}")
+        assert torch.equal(got, tk.tokens_embed_grad(G, t, V, 0.7))
+
+
+def test_two_streams_of_gradients(tk):
+    a = (rows((1, 500, 128), BF, 211), rows((1, 5_000, 128), BF, 212), ids(1, 500, 5_000, 213))
+    b = (rows((1, 400, 320), F16, 214), rows((1, 7_000, 320), F16, 215), ids(1, 400, 7_000, 216))
+
+    def go(X, W, t):
+        _, _, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.1)
+        g = torch.ones(t.shape, device="cuda")
+        dX, dW = tk.tokens_logprobs_grad(X, W, t, lse, g, scale=0.1)
+        return dX, dW, tk.tokens_embed_grad(dX, t, W.shape[1])
+
+    want = [go(*s) for s in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(4):
+        for st, s in zip(streams, (a, b)):
+            with torch.cuda.stream(st):
+                got.append(go(*s))
+    torch.cuda.synchronize()
+    for i, r in enumerate(got):
+        for x, y in zip(r, want[i % 2]):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("D", [64, 256, 300])
+def test_gradients_captured_and_replayed(tk, D):
+    """On both ways of dz, with eager calls between the replays."""
+    M, V = 700, 900
+
+    def fresh(seed):
+        return rows((1, M, D), F16, seed), rows((1, V, D), F16, seed + 1), ids(1, M, V, seed + 2), \
+            rows((1, M), F32, seed + 3)
+
+    def go(X, W, t, g, ws):
+        _, ent, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.1, ws=ws)
+        return tk.tokens_logprobs_grad(X, W, t, lse, g, entropy=ent, grad_entropy=g, scale=0.1, ws=ws)
+
+    def make_ws():
+        return torch.empty(max(tk.logprobs_workspace_bytes(1, M, V, D, 0, F16),
+                               tk.logprobs_grad_workspace_bytes(1, M, V, D, F16)), dtype=torch.uint8,
+                           device="cuda")
+
+    s, ws = fresh(221), make_ws()
+    go(*fresh(225), make_ws())
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr):
+        outs = go(*s, ws)
+    for r in range(4):
+        new = fresh(231 + 4 * r)
+        for x, y in zip(s, new):
+            x.copy_(y)
+        gr.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(outs, go(*new, make_ws())):
+            assert torch.equal(x, y), r

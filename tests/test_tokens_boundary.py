@@ -143,7 +143,24 @@ def test_workspaces_never_shrink_as_positions_grow(lib, B, V, D, k):
 
 def test_largest_sizes_have_workspaces(lib):
     """Sizes near every limit at once: the arithmetic must not overflow."""
-    n = lib.tokens_logprobs_grad_workspace_bytes(65535, 1 << 24, 1 << 20, 8192, BF16)
-    assert n > 65535 * (1 << 24) * 8192 * 2  # at least a copy of X
+    n = lib.tokens_logprobs_grad_workspace_bytes(65535, (1 << 23) - 64, 1 << 20, 8192, BF16)
+    assert n > 65535 * ((1 << 23) - 64) * 8192 * 2  # at least a copy of X
     n = lib.tokens_logprobs_workspace_bytes(65535, 1 << 24, 1 << 20, 8191, 32, BF16)
     assert n > 65535 * (1 << 24) * 8192 * 2
+
+
+def test_gradients_of_too_many_positions_are_refused(lib):
+    for M in ((1 << 23) - 63, 1 << 24):
+        assert lib.tokens_logprobs_grad_workspace_bytes(1, M, 8, 16, BF16) == 0
+        assert lib.tokens_logprobs_grad(P, P, BF16, None, P, P, None, P, None, 1, M, 8, 16, 1.0, P, P, P,
+                                        1 << 62, None) == EUNSUP
+    assert lib.tokens_logprobs_grad_workspace_bytes(1, (1 << 23) - 64, 8, 16, BF16) > 0
+
+
+@pytest.mark.parametrize("D", [128, 130, 200, 256, 257])
+def test_gradient_workspaces_never_shrink(lib, D):
+    """Across the sizes where dz changes between being stored and not."""
+    sizes = [1, 64, 100, 1000, 1025, 2047, 2048, 2049, 4096, 8191, 8192, 8193, 20_000, 100_000, 1 << 20]
+    for V in sizes:
+        got = [lib.tokens_logprobs_grad_workspace_bytes(1, M, V, D, BF16) for M in sizes]
+        assert got == sorted(got), (V, got)
