@@ -1009,25 +1009,20 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
     }
     __syncthreads();
     const uint16_t* p = in + r0 * D;
-    if (D % 8 == 0) {
-      const int rc = D / 8, n = nr * rc;
-      for (int i0 = tid; i0 < n; i0 += 4 * 512) {
-        uint4 q[4];
+    const int rc = D / 8, n = nr * rc;  // (D: the padded rows')
+    for (int i0 = tid; i0 < n; i0 += 4 * 512) {
+      uint4 q[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          q[u] = *reinterpret_cast<const uint4*>(p + (int64_t)min(i0 + u * 512, n - 1) * 8);
+      for (int u = 0; u < 4; ++u)
+        q[u] = *reinterpret_cast<const uint4*>(p + (int64_t)min(i0 + u * 512, n - 1) * 8);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const uint32_t x[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
-          uint32_t m = 0;
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t x[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
+        uint32_t m = 0;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) m = max(m, max(one(x[e]), one(x[e] >> 16)));
-          mag = max(mag, part[min(i0 + u * 512, n - 1) / rc] ? m : 0u);
-        }
+        for (int e = 0; e < 4; ++e) m = max(m, max(one(x[e]), one(x[e] >> 16)));
+        mag = max(mag, part[min(i0 + u * 512, n - 1) / rc] ? m : 0u);
       }
-    } else {
-      for (int i = tid; i < nr * D; i += 512)
-        if (part[i / D]) mag = max(mag, one(p[i]));
     }
     __syncthreads();
   }
@@ -1076,8 +1071,8 @@ __device__ __forceinline__ float4 grad_scales(const float4* stats, int n, float4
   return make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_14(o.y), up_to_2_14(o.z), 0.f);
 }
 
-// Transposed fp16 copies: in [nb, R, C] rows r0 .. r0 + nr - 1 of each instance, times a
-// factor, -> out [nb, C, ldo], zeros up to np.  Rows that take no part become zeros: of X
+// Transposed fp16 copies: in [nb, R, ld] rows r0 .. r0 + nr - 1 of each instance, times a
+// factor, -> out [nb, C, ldo] (C of their ld elements), zeros up to np.  Rows that take no part become zeros: of X
 // those without a gradient (the others times gs over the largest too), of W the forbidden
 // tokens.  64 x 64 values at a time: a thread reads 8 columns of two rows and stores them
 // in LDS as pairs of rows, and writes 8 rows of two columns.
@@ -1091,7 +1086,7 @@ struct CopyJob {
   bool mixed; // columns 16 t + 8 h + i hold rows 16 t + 8 (i / 4) + 4 h + i % 4
 };
 template <int DT>
-__global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
+__global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C, int ld,
                                                    const float4* __restrict__ stats, int nstats,
                                                    float4* __restrict__ scales) {
   __shared__ float4 sh[4];
@@ -1118,14 +1113,8 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C,
       alignas(16) uint16_t x8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       const int c = ct + 8 * c8;
       if (f != 0.f && c < C) {
-        const uint16_t* p = j.in + (b * j.R + j.r0 + r) * C + c;
-        if (C % 8 == 0) {
-          *reinterpret_cast<uint4*>(x8) = *reinterpret_cast<const uint4*>(p);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (c + e < C) x8[e] = p[e];
-        }
+        *reinterpret_cast<uint4*>(x8) =
+            *reinterpret_cast<const uint4*>(j.in + (b * j.R + j.r0 + r) * ld + c);
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -1488,8 +1477,8 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
   hipError_t e;
   const char *X = (const char*)a.X, *W = (const char*)a.W;
   if (w.Dk != a.D) {
-    if ((e = launch_pad_rows(X, a.B * a.M, a.D, w.Dk, 2, w.xpad, s)) != hipSuccess) return e;
-    if ((e = launch_pad_rows(W, a.B * a.V, a.D, w.Dk, 2, w.wpad, s)) != hipSuccess) return e;
+    if ((e = launch_pad_both(X, a.B * a.M, w.xpad, W, a.B * a.V, w.wpad, a.D, s)) != hipSuccess)
+      return e;
     X = (const char*)w.xpad;
     W = (const char*)w.wpad;
   }
@@ -1672,19 +1661,19 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   hipError_t e;
   const char *X = (const char*)a.X, *W = (const char*)a.W;
   if (w.Dk != a.D) {
-    if ((e = launch_pad_rows(X, a.B * a.M, a.D, w.Dk, 2, w.xpad, s)) != hipSuccess) return e;
-    if ((e = launch_pad_rows(W, a.B * a.V, a.D, w.Dk, 2, w.wpad, s)) != hipSuccess) return e;
+    if ((e = launch_pad_both(X, a.B * a.M, w.xpad, W, a.B * a.V, w.wpad, a.D, s)) != hipSuccess)
+      return e;
     X = (const char*)w.xpad;
     W = (const char*)w.wpad;
   }
   const int64_t lm = grad_ld(w.Mp);
   // blocks of about 64 KiB of rows, at most STATS_WGS / 2 workgroups for each of X and W
-  const int64_t rb = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / a.D));
+  const int64_t rb = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / w.Dk));
   const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
   const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
   grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
-      (const uint16_t*)a.X, (const uint16_t*)a.W, a.target, a.lse, a.entropy, a.g, a.h, a.bias, a.M,
-      (int)a.V, (int)a.D, (int)rb, (int)nx, w.rows, w.stats);
+      (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias, a.M,
+      (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);
@@ -1693,12 +1682,12 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
       const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
-      const CopyJob jx{(const uint16_t*)a.X + b0 * a.M * a.D, a.M, 0, a.M, w.Mp, lm, rg, nullptr,
+      const CopyJob jx{(const uint16_t*)X + b0 * a.M * w.Dk, a.M, 0, a.M, w.Mp, lm, rg, nullptr,
                        (uint16_t*)w.xt, v0 ? 0 : (int)(w.Mp / 64), w.narrow};
-      const CopyJob jw{(const uint16_t*)a.W + b0 * a.V * a.D, a.V, v0, nv, vp, lv, nullptr, bias,
+      const CopyJob jw{(const uint16_t*)W + b0 * a.V * w.Dk, a.V, v0, nv, vp, lv, nullptr, bias,
                        (uint16_t*)w.wt, (int)(vp / 64), w.narrow};
       copy_kernel<DT><<<dim3((unsigned)(jx.tiles + jw.tiles), (unsigned)((a.D + 63) / 64), (unsigned)nb),
-                        256, 0, s>>>(jx, jw, (int)a.D, w.stats + b0 * wgs, (int)wgs, scales);
+                        256, 0, s>>>(jx, jw, (int)a.D, (int)w.Dk, w.stats + b0 * wgs, (int)wgs, scales);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       if (w.narrow) {  // all instances and table rows at once
         if ((e = launch_narrow<DT>(a, w, X, W, scales, lm, lv, s)) != hipSuccess) return e;

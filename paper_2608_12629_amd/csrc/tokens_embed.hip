@@ -441,7 +441,59 @@ hipError_t launch_sums_wt(const void* G, int64_t B, int64_t M, int64_t V, int64_
              : launch_sums_dt<DT, WT, false>(G, B, M, V, D, scale, accumulate, dW, w, s);
 }
 
+// ---- rows of no whole number of 16-byte chunks ----------------------------------------
+struct PadJob {
+  const uint16_t* in;
+  uint4* out;
+  int64_t chunks, total;  // 16-byte chunks of the copy, elements of the rows
+};
+constexpr int PAD_CHUNKS = 2048;  // of a workgroup
+
+// A thread makes 16-byte chunks of the copy of 32-bit words, which start wherever a row
+// does; the workgroups past the first nx are w's.  Bound by HBM: 43,047 rows of 1,331
+// elements 43 us (5.3 TB/s read and written; a workgroup per row or so: 185).
+__global__ __launch_bounds__(256) void pad_kernel(PadJob x, PadJob w, int D, int ch, int64_t nx) {
+  const bool is_x = (int64_t)blockIdx.x < nx;
+  const PadJob j = is_x ? x : w;
+  const int64_t base = ((int64_t)blockIdx.x - (is_x ? 0 : nx)) * PAD_CHUNKS, row0 = base / ch;
+  const uint32_t rem0 = (uint32_t)(base - row0 * ch);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(j.in);
+#pragma unroll 4
+  for (int u = 0; u < PAD_CHUNKS / 256; ++u) {
+    const uint32_t at = u * 256 + threadIdx.x, rem = rem0 + at, r = rem / (uint32_t)ch;
+    if (base + at >= j.chunks) return;
+    const int c = (int)(rem - r * ch) * 8, n = min(8, D - c);
+    const int64_t e = (row0 + r) * D + c;
+    uint32_t v[4];
+    if (e + 9 <= j.total) {
+      uint32_t x[5];
+#pragma unroll
+      for (int i = 0; i < 5; ++i) x[i] = i < 4 || (e & 1) ? words[(e >> 1) + i] : 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = e & 1 ? x[i] >> 16 | x[i + 1] << 16 : x[i];
+        if (2 * i + 1 >= n) v[i] = 2 * i < n ? v[i] & 0xffffu : 0;  // the next row's
+      }
+    } else {  // the last chunks
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        v[i] = (2 * i < n ? j.in[e + 2 * i] : 0u) | (2 * i + 1 < n ? (uint32_t)j.in[e + 2 * i + 1] << 16 : 0u);
+    }
+    j.out[base + at] = make_uint4(v[0], v[1], v[2], v[3]);
+  }
+}
+
 }  // namespace
+
+hipError_t launch_pad_both(const void* X, int64_t xrows, void* xpad, const void* W, int64_t wrows,
+                           void* wpad, int64_t D, hipStream_t s) {
+  const int64_t ch = (D + 7) / 8;
+  const PadJob x{(const uint16_t*)X, (uint4*)xpad, xrows * ch, xrows * D};
+  const PadJob w{(const uint16_t*)W, (uint4*)wpad, wrows * ch, wrows * D};
+  const int64_t nx = (x.chunks + PAD_CHUNKS - 1) / PAD_CHUNKS, nw = (w.chunks + PAD_CHUNKS - 1) / PAD_CHUNKS;
+  pad_kernel<<<dim3((unsigned)(nx + nw)), 256, 0, s>>>(x, w, (int)D, (int)ch, nx);
+  return hipGetLastError();
+}
 
 hipError_t launch_embed(const void* W, int dt, const int32_t* idx, int64_t B, int64_t M, int64_t V,
                         int64_t D, float scale, void* out, hipStream_t s) {

@@ -36,6 +36,10 @@ hipError_t launch_token_sort(const int32_t* idx, int64_t B, int64_t M, int64_t V
 hipError_t launch_embed(const void* W, int dt, const int32_t* idx, int64_t B, int64_t M, int64_t V,
                         int64_t D, float scale, void* out, hipStream_t s);
 
+// Copies of 16-bit rows of D elements, X's and W's, in rows of the next multiple of 8.
+hipError_t launch_pad_both(const void* X, int64_t xrows, void* xpad, const void* W, int64_t wrows,
+                           void* wpad, int64_t D, hipStream_t s);
+
 struct EmbedGradWs {
   TokenSort sort;
   float* carry;  // [B, slices, 2, D] sums of runs cut by slice ends
