@@ -941,14 +941,31 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
   }
 }
 
+// Eight products more.
+template <int DT>
+__device__ __forceinline__ float dot_chunk(const uint4& x, const uint4& y, float z) {
+  const uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    z = __builtin_fmaf(Elem<DT>::widen((uint16_t)a[i]), Elem<DT>::widen((uint16_t)b[i]), z);
+    z = __builtin_fmaf(Elem<DT>::widen((uint16_t)(a[i] >> 16)), Elem<DT>::widen((uint16_t)(b[i] >> 16)), z);
+  }
+  return z;
+}
+
 // ---- gradient ------------------------------------------------------------------
 // dz and the copies of X and W that the two products read are fp16 for both storage
 // types: 11 significant bits against bf16's 8 make dz's rounding an eighth, below that
 // of the results (bf16 dz: dX and dW off by 2.4e-3 of their norm, 1.7e-3 being their own
-// rounding; fp16: 1.7e-3).  Powers of two keep all three in range: each row's dz is
-// stored over gs, at or above max(|g|, |h|), and DZ_UP times larger; X (times gs over
-// the largest gs) and W times what brings their largest value just below 2^14, where
-// fp16 holds every bf16 or fp16 value down to 2^-28 of that exactly.
+// rounding; fp16: 1.7e-3).  All three are kept in range: each row's dz is stored over gs
+// and DZ_UP times larger; X (times gs over the largest gs) and W times the power of two
+// that brings their largest value just below 2^14, where fp16 holds every bf16 or fp16
+// value down to 2^-28 of that exactly.  gs is a power of two at or above max(|g|, |h|);
+// for fp16 rows, whose results are rounded no more coarsely than dz, it is dz of the
+// target wherever that is the largest of the row.  Its rounding, which would be one
+// relative error of a whole row of dX, then vanishes, and X's copies, rounded each for
+// itself, bring less into dW (1 position, 8 x 8,931 x 586: dX and dW off by 3.5e-4 ->
+// 2.2e-4, 2.1e-4 being their own rounding).
 constexpr float DZ_UP = 2048.f;
 
 // What each position's gradient needs, and the largest gs and magnitudes: X's of the
@@ -959,10 +976,11 @@ template <int DT>
 __global__ __launch_bounds__(512) void grad_rows_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
     const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
-    const float* __restrict__ h, const float* __restrict__ bias, int64_t M, int V, int D, int rb, int nx,
-    RowGrad* __restrict__ out, float4* __restrict__ stats) {
+    const float* __restrict__ h, const float* __restrict__ bias, float scale, int64_t M, int V, int D,
+    int rb, int nx, RowGrad* __restrict__ out, float4* __restrict__ stats) {
   __shared__ float sh[8][2];
   __shared__ bool part[512];
+  __shared__ float zt_s[DT == DT_F16 ? 512 : 1];
   const int64_t b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const bool is_x = (int)blockIdx.x < nx;
@@ -977,6 +995,38 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
   };
   for (int64_t r0 = (is_x ? blockIdx.x : blockIdx.x - nx) * (int64_t)rb; r0 < rows; r0 += nblk * rb) {
     const int nr = (int)min<int64_t>(rb, rows - r0);
+    if constexpr (DT == DT_F16) {
+      if (is_x) {
+        // the targets' scores: `lpr` lanes a row, four rows of each at a time
+        const int ch = D / 8, lpr = ch > 32 ? 64 : ch > 16 ? 32 : ch > 8 ? 16 : 8;
+        const int step = 512 / lpr, l = tid % lpr;
+        for (int q0 = tid / lpr; q0 < nr; q0 += 4 * step) {
+          int t[4];
+          float z[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            t[u] = target[b * M + r0 + min(q0 + u * step, nr - 1)];
+            if ((unsigned)t[u] >= (unsigned)V) t[u] = 0;  // (not used)
+          }
+          for (int c = l; c < ch; c += lpr) {
+            uint4 x[4], y[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              x[u] = reinterpret_cast<const uint4*>(in + (r0 + min(q0 + u * step, nr - 1)) * D)[c];
+              y[u] = reinterpret_cast<const uint4*>(W + (b * V + t[u]) * D)[c];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) z[u] = dot_chunk<DT>(x[u], y[u], z[u]);
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            for (int m = 1; m < lpr; m <<= 1) z[u] += __shfl_xor(z[u], m);
+            if (l == 0 && q0 + u * step < nr) zt_s[q0 + u * step] = scale * z[u];
+          }
+        }
+      }
+      __syncthreads();
+    }
     if (tid < nr) {
       if (is_x) {
         const int64_t i = b * M + r0 + tid;
@@ -992,7 +1042,26 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         r.gs = 1.f;
         r.pad = 0;
         const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
-        if (r.active && big <= __FLT_MAX__) {
+        float u = 0.f;  // dz of the target, where it is the row's largest
+        if constexpr (DT == DT_F16) {
+          if (r.active && r.target >= 0) {
+            const float z = zt_s[tid] + (bias ? bias[b * V + r.target] : 0.f);
+            const float lp = __builtin_fminf(z - r.lse, 0.f), p = __expf(lp);
+            if (r.h == 0.f) {
+              u = r.g * __builtin_fmaxf(1.f - p, 0x1p-8f);
+            } else {
+              u = r.g * (1.f - p) - (p > 0.f ? r.h * p * (lp + r.ent) : 0.f);
+              if (__builtin_fabsf(u) < 0.25f * big) u = 0.f;
+            }
+            const float a = __builtin_fabsf(u);
+            if (!(a > 0x1p-100f && a < 0x1p100f && big < 0x1p100f)) u = 0.f;
+          }
+        }
+        if (u != 0.f) {
+          r.gs = u;
+          r.g /= u;
+          r.h /= u;
+        } else if (r.active && big <= __FLT_MAX__) {
           int e;
           (void)frexpf(big, &e);
           e = min(max(e, -120), 120);
@@ -1667,13 +1736,15 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     W = (const char*)w.wpad;
   }
   const int64_t lm = grad_ld(w.Mp);
-  // blocks of about 64 KiB of rows, at most STATS_WGS / 2 workgroups for each of X and W
-  const int64_t rb = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / w.Dk));
+  // blocks of about 64 KiB of rows, at most STATS_WGS / 2 workgroups for each of X and W;
+  // for fp16, whose rows wait for the targets' scores, smaller ones while there are few
+  const int64_t full = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / w.Dk));
+  const int64_t rb = DT == DT_F16 ? std::min(full, std::max<int64_t>(16, a.B * std::max(a.M, a.V) / 256)) : full;
   const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
   const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
   grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
-      (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias, a.M,
-      (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
+      (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias,
+      a.scale, a.M, (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);

@@ -154,11 +154,12 @@ constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
 constexpr int64_t LP_NARROW = 256, LP_NARROW_SCORES = 1 << 25;
 constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
 struct RowGrad {  // one position
-  float g, h;     // gradients of the log probability (>= 0) and the entropy, over `gs`
+  float g, h;     // gradients of the log probability (>= 0 without
+                  // gradients of entropies) and the entropy, over `gs`
   float lse, ent;
   int target;     // -1: none
   int active;     // takes part at all
-  float gs;       // a power of two with g's sign: what g, h and so dz of this row are divided by
+  float gs;       // what g, h and so dz of this row are divided by
   int pad;
 };
 // Elements from row to row of dz and the copies: 128 bytes past a multiple of 1 KiB, so

@@ -110,6 +110,8 @@ def grads(X, W, target, g, h=None, scale=1.0, bias=None):
         top = gs.amax(1, keepdim=True)
         per = torch.where(gs > 0, dz.abs() / gs.clamp(min=1e-300), 0.0).sum(1).unsqueeze(-1)
         eW = eW + abs(scale) * per * top * 2.0 ** -25
+        # X times a row's factor, no power of two, is rounded too: half a step of each product
+        eW = eW + half(dt) * torch.matmul(dzt.abs() + et, Xd.abs()) * abs(scale)
     tiny = torch.finfo(dt).smallest_normal * half(dt) * 2
     eX = eX + half(dt) * (dX.abs() + eX) + tiny
     eW = eW + half(dt) * (dW.abs() + eW) + tiny
