@@ -72,7 +72,7 @@ __device__ __forceinline__ T& nt_at(char* base, int off) {
   return *reinterpret_cast<T*>(base + off);
 }
 
-template <int TCW>
+constexpr int TCW = 2;  // tiles of 32 of A's rows that a wave has
 struct NtSize {
   static constexpr int BA = 128 * TCW;      // rows of A in a block
   static constexpr int AB = BA * 128;       // bytes of A in a stage
@@ -91,14 +91,13 @@ struct NtIn {
   int nA, nB, a0, b0, c0, c1, nblk;
 };
 
-template <int TCW>
 struct NtFrag {
   uint4 a[TCW], b[4];
 };
 
-template <int DT, int TCW>
+template <int DT>
 struct NtLoop {
-  using Z = NtSize<TCW>;
+  using Z = NtSize;
   NtIn in;
   // the stage to load next: block iblk, stage id of it; each operand's first row and
   // chunk of that stage, and the thread's offsets from it (rows clamped)
@@ -160,7 +159,7 @@ struct NtLoop {
     }
   }
 
-  __device__ __forceinline__ void read(NtFrag<TCW>& f, char* buf, int i) {  // i-th fragment
+  __device__ __forceinline__ void read(NtFrag& f, char* buf, int i) {  // i-th fragment
     if (i < TCW) f.a[i < TCW ? i : 0] = nt_at<uint4>(buf, (wc * TCW + i) * 4096);
     else f.b[i < TCW ? 0 : i - TCW] = nt_at<uint4>(buf, Z::AB + (wp * 4 + i - TCW) * 4096);
   }
@@ -173,7 +172,7 @@ struct NtLoop {
   // cycles an MFMA, so what stands between two of them is free; in a block of its own,
   // after the barrier and before the MFMAs, it cost both waves of a SIMD the same idle
   // cycles.
-  __device__ __forceinline__ void step(f32x16 (&acc)[4][TCW], const NtFrag<TCW>& f, NtFrag<TCW>& g,
+  __device__ __forceinline__ void step(f32x16 (&acc)[4][TCW], const NtFrag& f, NtFrag& g,
                                        char* buf, char* ahead, bool load) {
     constexpr int N = 4 * TCW, R = TCW + 4;
 #pragma unroll
@@ -195,8 +194,8 @@ struct NtLoop {
   // stage s + 1 and the loads of stage s + 2 (`load`) into this stage's buffer.  Past the
   // last stage the reads bring values that nobody uses; one path for all stages keeps
   // the accumulators in their registers.
-  __device__ __forceinline__ void stage(int s, bool load, f32x16 (&acc)[4][TCW], NtFrag<TCW>& f0,
-                                        NtFrag<TCW>& f1) {
+  __device__ __forceinline__ void stage(int s, bool load, f32x16 (&acc)[4][TCW], NtFrag& f0,
+                                        NtFrag& f1) {
     char *cur = at(s), *nxt = at(s + 1);
     step(acc, f0, f1, step_at(cur, 1), nullptr, false);
     step(acc, f1, f0, step_at(cur, 2), nullptr, false);
@@ -218,7 +217,7 @@ struct NtLoop {
     if (1 < S) issue(at(1));
     if (1 < S) nt_wait_and_sync<Z::LOADS>();
     else nt_wait_and_sync<0>();
-    NtFrag<TCW> f0, f1;
+    NtFrag f0, f1;
 #pragma unroll
     for (int i = 0; i < TCW + 4; ++i) read(f0, step_at(at(0), 0), i);
     f32x16 acc[4][TCW];
@@ -327,7 +326,7 @@ struct ScoreArgs {
 
 template <int DT, bool BIAS, bool TOPK>
 __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
-  using Z = NtSize<2>;
+  using Z = NtSize;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   int mb, sp;
   int64_t b;
@@ -346,7 +345,7 @@ __global__ __launch_bounds__(NT_T, 1) void score_kernel(ScoreArgs a) {
   in.c0 = 0;
   in.c1 = a.chunks;
   in.nblk = blk1 - blk0;
-  NtLoop<DT, 2> loop;
+  NtLoop<DT> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   // per row: the target, its score, the bound (in LDS: registers are short)
@@ -523,10 +522,9 @@ struct FewArgs {
 
 // ONCE: the table is read past the caches, for ones beyond the 256 MiB of the last cache
 // (131,072 x 4,096: 214 -> 204 us; but 205 MB: 60 -> 62).
-template <int DT, int CB, bool BIAS, bool TOPK, bool ONCE>
-__global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
-  constexpr int LDR = 68;  // floats from position to position: 64 scores and 4 of padding
-  __shared__ __attribute__((aligned(16))) float red[4][16 * CB * LDR];
+constexpr int FEW_LD = 68;  // floats from position to position: 64 scores and 4 of padding
+template <int DT, int CB, bool ONCE>
+__device__ __forceinline__ void few_products(const FewArgs& a, float (&red)[4][16 * CB * FEW_LD]) {
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t b = blockIdx.y;
@@ -604,8 +602,17 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
   for (int i = 0; i < 4; ++i)
 #pragma unroll
     for (int j = 0; j < CB; ++j)
-      *reinterpret_cast<f32x4*>(&red[w][(16 * j + r16) * LDR + 16 * i + 4 * q4]) = acc[i][j];
+      *reinterpret_cast<f32x4*>(&red[w][(16 * j + r16) * FEW_LD + 16 * i + 4 * q4]) = acc[i][j];
   __syncthreads();
+}
+
+template <int DT, int CB, bool BIAS, bool TOPK, bool ONCE>
+__global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
+  __shared__ __attribute__((aligned(16))) float red[4][16 * CB * FEW_LD];
+  few_products<DT, CB, ONCE>(a, red);
+  const int tid = threadIdx.x;
+  const int64_t b = blockIdx.y;
+  const int v0 = blockIdx.x * 64, m0 = blockIdx.z * (16 * CB);
   // 16 / CB lanes a position, 4 CB columns each
   constexpr int TPM = 16 / CB, VPT = 4 * CB;
   const int ml = tid / TPM, part = tid % TPM, m = m0 + ml;
@@ -613,7 +620,7 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_kernel(FewArgs a) {
   float z[VPT], lm = NEG_INF;
 #pragma unroll
   for (int j = 0; j < VPT; j += 4) {
-    const int at = ml * LDR + part * VPT + j;
+    const int at = ml * FEW_LD + part * VPT + j;
     f32x4 x = (*reinterpret_cast<const f32x4*>(&red[0][at]) + *reinterpret_cast<const f32x4*>(&red[1][at])) +
               (*reinterpret_cast<const f32x4*>(&red[2][at]) + *reinterpret_cast<const f32x4*>(&red[3][at]));
 #pragma unroll
@@ -1226,7 +1233,7 @@ struct DzArgs {
 // finished stage's buffer, so that lines of both results are written whole.
 template <int DT, bool BIAS, bool ENT>
 __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
-  using Z = NtSize<2>;
+  using Z = NtSize;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   __shared__ float4 row_s[LP_BB];  // c0, c1, lse in units of log 2, g
   __shared__ int tgt_s[LP_BB];     // -1: none; -2: the row takes no part
@@ -1255,7 +1262,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     tgt_s[r] = rg.active ? rg.target : -2;
   }
   __syncthreads();
-  NtLoop<DT, 2> loop;
+  NtLoop<DT> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   const float c2 = a.scale * LOG2E;
@@ -1350,6 +1357,69 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   loop.template run<true>(epi);
 }
 
+// The same of few rows (see few_kernel, whose products these are): a lane has 4 CB
+// columns of a position, and the transpose goes through LDS to whole lines.  2 x 3,178 x
+// 1,472: the call 96 -> 42 us.
+template <int DT, int CB, bool BIAS, bool ENT>
+__global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
+    FewArgs a, const RowGrad* __restrict__ rows, uint16_t* __restrict__ dz, uint16_t* __restrict__ dzt,
+    int64_t lv, int64_t Vp, int64_t lm) {
+  __shared__ __attribute__((aligned(16))) float red[4][16 * CB * FEW_LD];
+  few_products<DT, CB, false>(a, red);
+  constexpr int TPM = 16 / CB, VPT = 4 * CB, LT = 72;  // LT: elements from column to column
+  const int tid = threadIdx.x, ml = tid / TPM, part = tid % TPM;
+  const int64_t b = blockIdx.y;
+  const int v0 = blockIdx.x * 64, m0 = blockIdx.z * (16 * CB), m = m0 + ml, vb = v0 + part * VPT;
+  RowGrad rg;
+  rg.active = 0;
+  if (m < a.M) rg = rows[b * a.M + m];
+  const float c0 = -DZ_UP * __builtin_fmaf(rg.h, rg.ent, rg.g), c1 = -DZ_UP * LN2 * rg.h;
+  const float lse2 = rg.lse * LOG2E, c2 = a.scale * LOG2E;
+  uint32_t y2[VPT / 2];
+#pragma unroll
+  for (int j = 0; j < VPT; j += 4) {
+    const int at = ml * FEW_LD + part * VPT + j;
+    const f32x4 x =
+        (*reinterpret_cast<const f32x4*>(&red[0][at]) + *reinterpret_cast<const f32x4*>(&red[1][at])) +
+        (*reinterpret_cast<const f32x4*>(&red[2][at]) + *reinterpret_cast<const f32x4*>(&red[3][at]));
+    float y[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int v = vb + j + r;
+      const float bz = BIAS && v < a.V ? a.bias[b * a.V + v] : 0.f;
+      float l;
+      if constexpr (BIAS)
+        l = __builtin_fmaf(__builtin_fmaf(x[r], a.scale, bz), LOG2E, -lse2);
+      else
+        l = __builtin_fmaf(x[r], c2, -lse2);
+      const float p = __builtin_amdgcn_exp2f(l);
+      y[r] = ENT ? p * __builtin_fmaf(__builtin_fmaxf(l, -1e30f), c1, c0) : p * c0;
+      if (v == rg.target) y[r] += DZ_UP * rg.g;
+      if (!rg.active || v >= a.V || bz == NEG_INF) y[r] = 0.f;
+    }
+    y2[j / 2] = half2_bits(y[0], y[1]);
+    y2[j / 2 + 1] = half2_bits(y[2], y[3]);
+  }
+  if (m < a.M) {
+    uint16_t* o = dz + (b * a.M + m) * lv + vb;
+#pragma unroll
+    for (int j = 0; j < VPT / 2; j += 2) *reinterpret_cast<uint2*>(o + 2 * j) = make_uint2(y2[j], y2[j + 1]);
+  }
+  __syncthreads();
+  uint16_t* tile = reinterpret_cast<uint16_t*>(&red[0][0]);
+#pragma unroll
+  for (int j = 0; j < VPT; ++j)
+    tile[(part * VPT + j) * LT + ml] = (uint16_t)(y2[j / 2] >> (j % 2 * 16));
+  __syncthreads();
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {  // eight positions of a column a thread, zeros past the last
+    const int at = u * 256 + tid, r = at / 8, c = at % 8;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (8 * c < 16 * CB) x = *reinterpret_cast<const uint4*>(&tile[r * LT + 8 * c]);
+    *reinterpret_cast<uint4*>(dzt + (b * Vp + v0 + r) * lm + m0 + 8 * c) = x;
+  }
+}
+
 // ---- the two products of the gradient ----------------------------------------------
 // out[r, d] = sum over c of At[d, c] Br[r, c]: At a transposed copy (D rows), Br dz or
 // its transpose.  Shares of the contraction go to `part` in fp32; whole ones are
@@ -1361,12 +1431,13 @@ struct OutArgs {
   int64_t ld;          // bytes of a row of either
   int64_t R, os;       // rows, rows between instances of the output
   int D, chunks, per;  // chunks of the contraction, stages of a share
+  int ldf;
   int splits, mode, lanes;
   float factor;
   const RowGrad* rows;   // dX: times gs of the row, over W's factor
   const float4* scales;  // dW (rows NULL): times the largest gs, over X's factor
   uint16_t* out;
-  float* f32;          // part [nb, splits, R, D] or acc [R, D]
+  float* f32;          // part [nb, splits, R, ldf] or acc [R, ldf]
   Raster grid;         // instances: the shares of each
 };
 
@@ -1375,45 +1446,53 @@ __device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b, int64_t
   return a.rows ? a.factor / s.z * a.rows[b * a.os + r].gs : a.factor / s.y * s.x;
 }
 
-// Eight consecutive results of a row (those below D) from `v`.
+// Eight consecutive results of a row (those below D) from `v`.  Rows of fp32 sums are
+// ldf (D's multiple of 8) elements apart.  16-bit rows of other widths begin at any
+// element: three aligned pairs and the two elements that are left (65 x 43,047 x 1,331:
+// one by one 372 -> 305 us).
 template <int DT>
 __device__ __forceinline__ void out_store(const OutArgs& a, int64_t b, int sp, int64_t r, int d,
                                           float (&v)[8]) {
   if (a.mode == OUT_16) {
     const float f = out_factor(a, b, r);
-    uint16_t* o = a.out + (b * a.os + r) * a.D + d;
+    const int64_t at = (b * a.os + r) * a.D + d;
+    uint16_t* o = a.out + at;
     alignas(16) uint16_t x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = Elem<DT>::narrow(v[e] * f);
     if (a.D % 8 == 0) {
       *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(x);
+    } else if (d + 8 <= a.D) {
+      const bool odd = at & 1;
+#pragma unroll
+      for (int e = 0; e < 3; ++e) {
+        const uint32_t even2 = x[2 * e] | (uint32_t)x[2 * e + 1] << 16;
+        const uint32_t odd2 = x[2 * e + 1] | (uint32_t)x[2 * e + 2] << 16;
+        *reinterpret_cast<uint32_t*>(o + 2 * e + (odd ? 1 : 0)) = odd ? odd2 : even2;
+      }
+      o[odd ? 0 : 6] = odd ? x[0] : x[6];
+      o[7] = x[7];
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (d + e < a.D) o[e] = x[e];
     }
   } else {
-    float* p = a.mode == OUT_PART ? a.f32 + ((b * a.splits + sp) * a.R + r) * a.D + d
-                                  : a.f32 + r * a.D + d;
-    if (a.D % 8 == 0) {
+    float* p = a.mode == OUT_PART ? a.f32 + ((b * a.splits + sp) * a.R + r) * a.ldf + d
+                                  : a.f32 + r * a.ldf + d;
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        f32x4 x = {v[e], v[e + 1], v[e + 2], v[e + 3]};
-        if (a.mode == OUT_ADD) x += *reinterpret_cast<const f32x4*>(p + e);
-        *reinterpret_cast<f32x4*>(p + e) = x;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (d + e < a.D) p[e] = a.mode == OUT_ADD ? p[e] + v[e] : v[e];
+    for (int e = 0; e < 8; e += 4) {
+      f32x4 x = {v[e], v[e + 1], v[e + 2], v[e + 3]};
+      if (a.mode == OUT_ADD) x += *reinterpret_cast<const f32x4*>(p + e);
+      *reinterpret_cast<f32x4*>(p + e) = x;
     }
   }
 }
 
 // (Both products in one launch: the workgroups past the first np are q's.)
-template <int DT, int TCW>
+template <int DT>
 __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int np) {
-  using Z = NtSize<TCW>;
+  using Z = NtSize;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   const bool is_p = (int)blockIdx.x < np;
   const OutArgs a = is_p ? p : q;
@@ -1434,7 +1513,7 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int 
   in.c0 = sp * a.per * 8;
   in.c1 = min(a.chunks, in.c0 + a.per * 8);
   in.nblk = 1;
-  NtLoop<DT_F16, TCW> loop;
+  NtLoop<DT_F16> loop;
   loop.init(in, smem);
   const int wp = loop.wp, wc = loop.wc;
   auto epi = [&](f32x16(&acc)[4][TCW], int, char*) {
@@ -1482,21 +1561,15 @@ __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, i
   o.mode = OUT_16;
   const int64_t br = min(i, n - 1) / dc, b = br / a.R, r = br % a.R;
   const int d = (int)(min(i, n - 1) % dc) * 8;
-  const float* from = a.f32 + (b * a.splits * a.R + r) * a.D + d;
+  const float* from = a.f32 + (b * a.splits * a.R + r) * a.ldf + d;
   float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int s = l; s < a.splits; s += a.lanes) {
-    const float* x = from + s * (a.R * a.D);
-    if (a.D % 8 == 0) {
+    const float* x = from + s * (a.R * a.ldf);
 #pragma unroll
-      for (int e = 0; e < 8; e += 4) {
-        const f32x4 y = *reinterpret_cast<const f32x4*>(x + e);
+    for (int e = 0; e < 8; e += 4) {
+      const f32x4 y = *reinterpret_cast<const f32x4*>(x + e);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[e + k] += y[k];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (d + e < a.D) v[e] += x[e];
+      for (int k = 0; k < 4; ++k) v[e + k] += y[k];
     }
   }
   for (int m = 1; m < a.lanes; m <<= 1) {
@@ -1649,19 +1722,17 @@ hipError_t launch_reduce(OutArgs& p, OutArgs& q, int64_t nb, hipStream_t s) {
 // Both products over nb instances: p's and q's contractions in `sp` and `sq` shares.
 template <int DT>
 hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, hipStream_t s) {
-  const bool narrow = p.D <= 128;
   auto plan = [&](OutArgs& a, int splits) {
     const int nst = (a.chunks + 7) / 8;
     a.per = (nst + splits - 1) / splits;
     a.splits = (nst + a.per - 1) / a.per;
-    a.grid = make_raster((a.D + (narrow ? 127 : 255)) / (narrow ? 128 : 256),
+    a.grid = make_raster((a.D + 255) / 256,
                          (a.R + LP_BB - 1) / LP_BB, nb * a.splits);
     return a.grid.blocks();
   };
   const int64_t np = plan(p, sp), nq = plan(q, sq);
   const dim3 grid((unsigned)(np + nq));
-  if (narrow) out_kernel<DT, 1><<<grid, NT_T, 0, s>>>(p, q, (int)np);
-  else out_kernel<DT, 2><<<grid, NT_T, 0, s>>>(p, q, (int)np);
+  out_kernel<DT><<<grid, NT_T, 0, s>>>(p, q, (int)np);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : launch_reduce<DT>(p, q, nb, s);
 }
@@ -1692,6 +1763,7 @@ hipError_t launch_narrow(const GradArgs& a, const GradWs& g, const char* X, cons
   x.rows = g.rows;
   x.scale = a.scale;
   x.out.D = (int)a.D;
+  x.out.ldf = (int)g.Dk;
   x.out.factor = (a.h ? a.scale : -a.scale) / DZ_UP;  // (see dz_of)
   x.out.scales = scales;
   NarrowArgs w = x;
@@ -1718,11 +1790,33 @@ hipError_t launch_narrow(const GradArgs& a, const GradWs& g, const char* X, cons
   side(x, X, a.M, W, a.V, g.wt, lv, g.sx, a.dX, g.part);
   x.out.rows = g.rows;
   side(w, W, a.V, X, a.M, g.xt, lm, g.sw, a.dW,
-       g.part + (x.out.mode == OUT_PART ? a.B * g.sx * a.M * a.D : 0));
+       g.part + (x.out.mode == OUT_PART ? a.B * g.sx * a.M * g.Dk : 0));
   const hipError_t e = a.D <= 64 ? launch_narrow_dd<DT, 64>(a, x, w, s)
                        : a.D <= 128 ? launch_narrow_dd<DT, 128>(a, x, w, s)
                                     : launch_narrow_dd<DT, 256>(a, x, w, s);
   return e != hipSuccess ? e : launch_reduce<DT>(x.out, w.out, a.B, s);
+}
+
+template <int DT, int CB>
+hipError_t launch_few_dz(const DzArgs& d, int64_t nb, bool ent, hipStream_t s) {
+  FewArgs q{};
+  q.X = d.X;
+  q.W = d.W;
+  q.bias = d.bias;
+  q.M = (int)d.M;
+  q.V = d.V;
+  q.chunks = d.chunks;
+  q.ld = d.ld;
+  q.scale = d.scale;
+  const dim3 grid((unsigned)(d.Vp / 64), (unsigned)nb, (unsigned)((d.M + 16 * CB - 1) / (16 * CB)));
+  if (d.bias) {
+    if (ent) few_dz_kernel<DT, CB, true, true><<<grid, 256, 0, s>>>(q, d.rows, d.dz, d.dzt, d.lv, d.Vp, d.lm);
+    else few_dz_kernel<DT, CB, true, false><<<grid, 256, 0, s>>>(q, d.rows, d.dz, d.dzt, d.lv, d.Vp, d.lm);
+  } else {
+    if (ent) few_dz_kernel<DT, CB, false, true><<<grid, 256, 0, s>>>(q, d.rows, d.dz, d.dzt, d.lv, d.Vp, d.lm);
+    else few_dz_kernel<DT, CB, false, false><<<grid, 256, 0, s>>>(q, d.rows, d.dz, d.dzt, d.lv, d.Vp, d.lm);
+  }
+  return hipGetLastError();
 }
 
 template <int DT>
@@ -1784,21 +1878,28 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       d.Mp = w.Mp;
       d.lv = lv;
       d.lm = lm;
-      const int64_t nmb = (a.M + LP_BB - 1) / LP_BB, nvb = (nv + 255) / 256;
-      d.grid = make_raster(score_splits(nmb, nb, nvb, (w.Dk + LP_DC - 1) / LP_DC), nmb, nb);
-      const dim3 grid((unsigned)d.grid.blocks());
-      if (a.bias) {
-        if (a.h) dz_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(d);
-        else dz_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(d);
+      if (nv == a.V && score_few(nb, a.M, a.V, w.Dk)) {
+        e = a.M <= 16 ? launch_few_dz<DT, 1>(d, nb, a.h, s) : a.M <= 32 ? launch_few_dz<DT, 2>(d, nb, a.h, s)
+                                                                      : launch_few_dz<DT, 4>(d, nb, a.h, s);
+        if (e != hipSuccess) return e;
       } else {
-        if (a.h) dz_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(d);
-        else dz_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(d);
+        const int64_t nmb = (a.M + LP_BB - 1) / LP_BB, nvb = (nv + 255) / 256;
+        d.grid = make_raster(score_splits(nmb, nb, nvb, (w.Dk + LP_DC - 1) / LP_DC), nmb, nb);
+        const dim3 grid((unsigned)d.grid.blocks());
+        if (a.bias) {
+          if (a.h) dz_kernel<DT, true, true><<<grid, NT_T, 0, s>>>(d);
+          else dz_kernel<DT, true, false><<<grid, NT_T, 0, s>>>(d);
+        } else {
+          if (a.h) dz_kernel<DT, false, true><<<grid, NT_T, 0, s>>>(d);
+          else dz_kernel<DT, false, false><<<grid, NT_T, 0, s>>>(d);
+        }
+        if ((e = hipGetLastError()) != hipSuccess) return e;
       }
-      if ((e = hipGetLastError()) != hipSuccess) return e;
 
       const bool whole = w.Vc >= a.V;  // one block of table rows
       OutArgs x{};
       x.D = (int)a.D;
+      x.ldf = (int)w.Dk;
       x.factor = a.scale / DZ_UP;
       x.scales = scales;
       OutArgs q = x;
@@ -1825,12 +1926,13 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.chunks = (int)(w.Mp / 8);
       q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
       q.mode = w.sw > 1 ? OUT_PART : OUT_16;
-      q.f32 = w.part + (x.mode == OUT_PART ? nb * w.sx * a.M * a.D : 0);
+      q.f32 = w.part + (x.mode == OUT_PART ? nb * w.sx * a.M * w.Dk : 0);
       if ((e = launch_out<DT>(x, whole ? w.sx : 1, q, w.sw, nb, s)) != hipSuccess) return e;
     }
     if (w.Vc < a.V) {  // dX from its fp32 sums
       OutArgs x{}, none{};
       x.D = (int)a.D;
+      x.ldf = (int)w.Dk;
       x.R = x.os = a.M;
       x.splits = 1;
       x.mode = OUT_PART;

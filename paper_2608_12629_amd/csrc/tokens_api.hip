@@ -139,14 +139,14 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   take(w.dzt, held);
   take(w.xt, (size_t)(B * D * (w.Mp + 64)) * 2);
   take(w.wt, (size_t)(B * D * (Vall + 64)) * 2);
-  take(w.accx, w.Vc < V ? (size_t)(M * D) * 4 : 0);
+  take(w.accx, w.Vc < V ? (size_t)(M * w.Dk) * 4 : 0);
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
-  const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * D * (Vall / 512), cap);
-  const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * D * (w.Mp / 512), cap);
+  const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * w.Dk * (Vall / 512), cap);
+  const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * w.Dk * (w.Mp / 512), cap);
   // narrow: at most narrow_wgs x 128 rows of a side in shares
-  const double ncap = (double)narrow_wgs(D) * 128 * (double)D;
-  const double nx = std::min((double)B * M * D * std::max<int64_t>(1, Vall / 256), ncap);
-  const double nw = std::min((double)B * V * D * std::max<int64_t>(1, w.Mp / 256), ncap);
+  const double ncap = (double)narrow_wgs(D) * 128 * (double)w.Dk;
+  const double nx = std::min((double)B * M * w.Dk * std::max<int64_t>(1, Vall / 256), ncap);
+  const double nw = std::min((double)B * V * w.Dk * std::max<int64_t>(1, w.Mp / 256), ncap);
   take(w.part, (size_t)(D <= 128 ? nx + nw : D <= LP_NARROW ? std::max(nx + nw, px + pw) : px + pw) * 4);
   w.total = take.o;
   return w;
