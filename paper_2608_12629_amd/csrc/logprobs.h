@@ -1441,9 +1441,12 @@ struct OutArgs {
   Raster grid;         // instances: the shares of each
 };
 
-__device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b, int64_t r) {
+// An instance's factor, but for dX's rows' gs: once for all results, as a load and a
+// division each time cost more than writing them (one position, 131,072 x 1,024: the
+// call 425 -> 406 us).
+__device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b) {
   const float4 s = a.scales[b];
-  return a.rows ? a.factor / s.z * a.rows[b * a.os + r].gs : a.factor / s.y * s.x;
+  return a.rows ? a.factor / s.z : a.factor / s.y * s.x;
 }
 
 // Eight consecutive results of a row (those below D) from `v`.  Rows of fp32 sums are
@@ -1451,10 +1454,10 @@ __device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b, int64_t
 // element: three aligned pairs and the two elements that are left (65 x 43,047 x 1,331:
 // one by one 372 -> 305 us).
 template <int DT>
-__device__ __forceinline__ void out_store(const OutArgs& a, int64_t b, int sp, int64_t r, int d,
+__device__ __forceinline__ void out_store(const OutArgs& a, float f, int64_t b, int sp, int64_t r, int d,
                                           float (&v)[8]) {
   if (a.mode == OUT_16) {
-    const float f = out_factor(a, b, r);
+    if (a.rows) f *= a.rows[b * a.os + r].gs;
     const int64_t at = (b * a.os + r) * a.D + d;
     uint16_t* o = a.out + at;
     alignas(16) uint16_t x[8];
@@ -1520,6 +1523,7 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int 
     // 32 rows by 32 TCW columns at a time through the wave's own LDS, so that lines are
     // written whole: row n's 16-byte unit c at c ^ (n & 7)
     __syncthreads();  // every wave has read its last stage
+    const float f = out_factor(a, b);
     char* sq = smem + loop.wave * (4096 * TCW);
     constexpr int LPR = 4 * TCW, RPI = 64 / LPR;  // lanes a row, rows a step
     const int d = in.a0 + wc * 32 * TCW + 8 * (lane % LPR);
@@ -1541,7 +1545,7 @@ __global__ __launch_bounds__(NT_T, 1) void out_kernel(OutArgs p, OutArgs q, int 
         for (int e = 0; e < 2; ++e)
           *reinterpret_cast<f32x4*>(v + 4 * e) =
               nt_at<f32x4>(sq, rl * (128 * TCW) + (((2 * (lane % LPR) + e) ^ (rl & 7)) << 4));
-        if (r < a.R && d < a.D) out_store<DT>(a, b, sp, r, d, v);
+        if (r < a.R && d < a.D) out_store<DT>(a, f, b, sp, r, d, v);
       }
     }
   };
@@ -1576,7 +1580,7 @@ __global__ __launch_bounds__(256) void out_reduce_kernel(OutArgs p, OutArgs q, i
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += __shfl_xor(v[e], m);
   }
-  if (l == 0 && i < n) out_store<DT>(o, b, 0, r, d, v);
+  if (l == 0 && i < n) out_store<DT>(o, out_factor(o, b), b, 0, r, d, v);
 }
 
 #include "logprobs_narrow.h"

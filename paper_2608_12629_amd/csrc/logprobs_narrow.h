@@ -320,6 +320,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   // 32 rows by 64 columns at a time through LDS, whole lines out, as in out_kernel
   __syncthreads();
   char* sq = smem + wave * 8192;
+  const float f = out_factor(a.out, b);
 #pragma unroll
   for (int i = 0; i < DD / 64; ++i) {
 #pragma unroll
@@ -339,7 +340,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
       for (int e = 0; e < 2; ++e)
         *reinterpret_cast<f32x4*>(v + 4 * e) =
             nt_at<f32x4>(sq, rl * 256 + (((2 * (lane & 7) + e) ^ (rl & 7)) << 4));
-      if (own0 + rl < a.nown && d < a.out.D) out_store<DT>(a.out, b, sp, own0 + rl, d, v);
+      if (own0 + rl < a.nown && d < a.out.D) out_store<DT>(a.out, f, b, sp, own0 + rl, d, v);
     }
   }
 }
