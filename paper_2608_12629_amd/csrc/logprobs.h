@@ -967,12 +967,13 @@ __device__ __forceinline__ float dot_chunk(const uint4& x, const uint4& y, float
 // rounding; fp16: 1.7e-3).  All three are kept in range: each row's dz is stored over gs
 // and DZ_UP times larger; X (times gs over the largest gs) and W times the power of two
 // that brings their largest value just below 2^14, where fp16 holds every bf16 or fp16
-// value down to 2^-28 of that exactly.  gs is a power of two at or above max(|g|, |h|);
-// for fp16 rows, whose results are rounded no more coarsely than dz, it is dz of the
-// target wherever that is the largest of the row.  Its rounding, which would be one
-// relative error of a whole row of dX, then vanishes, and X's copies, rounded each for
-// itself, bring less into dW (1 position, 8 x 8,931 x 586: dX and dW off by 3.5e-4 ->
-// 2.2e-4, 2.1e-4 being their own rounding).
+// value down to 2^-28 of that exactly.  gs is a power of two at or above max(|g|, |h|).
+// dz's rounding is then, with fp16 results, as large as theirs, and one relative error of
+// a row wherever one dz, the target's, makes most of it: over many rows 1.4 times the
+// results' own rounding, over few up to 2.3 times (1 position, 8 x 8,931 x 586: 3.5e-4).
+// So for up to LP_EXACT fp16 positions gs is dz of the target wherever that is the
+// largest: it has no rounding then, and X's copies, rounded each for itself, bring less
+// into dW (the same: 2.2e-4, 2.1e-4 being the results' own rounding).
 constexpr float DZ_UP = 2048.f;
 
 // What each position's gradient needs, and the largest gs and magnitudes: X's of the
@@ -983,8 +984,8 @@ template <int DT>
 __global__ __launch_bounds__(512) void grad_rows_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
     const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
-    const float* __restrict__ h, const float* __restrict__ bias, float scale, int64_t M, int V, int D,
-    int rb, int nx, RowGrad* __restrict__ out, float4* __restrict__ stats) {
+    const float* __restrict__ h, const float* __restrict__ bias, float scale, bool exact, int64_t M,
+    int V, int D, int rb, int nx, RowGrad* __restrict__ out, float4* __restrict__ stats) {
   __shared__ float sh[8][2];
   __shared__ bool part[512];
   __shared__ float zt_s[DT == DT_F16 ? 512 : 1];
@@ -1002,7 +1003,7 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
   };
   for (int64_t r0 = (is_x ? blockIdx.x : blockIdx.x - nx) * (int64_t)rb; r0 < rows; r0 += nblk * rb) {
     const int nr = (int)min<int64_t>(rb, rows - r0);
-    if constexpr (DT == DT_F16) {
+    if (DT == DT_F16 && exact) {
       if (is_x) {
         // the targets' scores: `lpr` lanes a row, four rows of each at a time
         const int ch = D / 8, lpr = ch > 32 ? 64 : ch > 16 ? 32 : ch > 8 ? 16 : 8;
@@ -1050,7 +1051,7 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         r.pad = 0;
         const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
         float u = 0.f;  // dz of the target, where it is the row's largest
-        if constexpr (DT == DT_F16) {
+        if (DT == DT_F16 && exact) {
           if (r.active && r.target >= 0) {
             const float z = zt_s[tid] + (bias ? bias[b * V + r.target] : 0.f);
             const float lp = __builtin_fminf(z - r.lse, 0.f), p = __expf(lp);
@@ -1835,14 +1836,15 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   }
   const int64_t lm = grad_ld(w.Mp);
   // blocks of about 64 KiB of rows, at most STATS_WGS / 2 workgroups for each of X and W;
-  // for fp16, whose rows wait for the targets' scores, smaller ones while there are few
+  // smaller ones for the few rows that wait for their targets' scores
+  const bool exact = DT == DT_F16 && a.B * a.M <= LP_EXACT;
   const int64_t full = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / w.Dk));
-  const int64_t rb = DT == DT_F16 ? std::min(full, std::max<int64_t>(16, a.B * std::max(a.M, a.V) / 256)) : full;
+  const int64_t rb = exact ? std::min(full, std::max<int64_t>(16, a.V / 256)) : full;
   const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
   const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
   grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
       (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias,
-      a.scale, a.M, (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
+      a.scale, exact, a.M, (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);

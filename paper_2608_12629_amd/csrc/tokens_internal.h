@@ -152,6 +152,7 @@ struct LogprobsArgs {
 // and both products read it and transposed fp16 copies of X and W.
 constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
 constexpr int64_t LP_NARROW = 256, LP_NARROW_SCORES = 1 << 25;
+constexpr int64_t LP_EXACT = 64;     // fp16 positions up to which a target's dz is exact
 constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
 struct RowGrad {  // one position
   float g, h;     // gradients of the log probability (>= 0 without

@@ -675,3 +675,17 @@ def test_gradients_captured_and_replayed(tk, D):
         torch.cuda.synchronize()
         for x, y in zip(outs, go(*new, make_ws())):
             assert torch.equal(x, y), r
+
+
+@pytest.mark.parametrize("B,M,V,D", [(8, 1, 8_931, 586), (1, 12, 4_477, 704), (1, 64, 300, 64), (1, 65, 300, 64),
+                                     (1, 3, 50, 1_000)])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_fp16_gradients_of_few_positions(tk, B, M, V, D, entropy):
+    """Rows made mostly by one token's dz: forms of a target's dz of any size next to 1 - p."""
+    X, W, t = rows((B, M, D), F16, 241), rows((B, V, D), F16, 242), ids(B, M, V, 243, none=0.1)
+    for lean in (0.0, 0.5, 3.0):  # p of the target from near 0 to near 1
+        at = torch.where((t >= 0) & (t < V), t, 0).long().unsqueeze(-1).expand(-1, -1, D)
+        Y = (X.float() + lean * torch.gather(W, 1, at).float()).half()
+        g = rows((B, M), F32, 244) * torch.logspace(0, -4, M, device="cuda")
+        h = rows((B, M), F32, 245, 0.2) if entropy else None
+        check_grads(tk, Y, W, t, g, h, 2.0 / D ** 0.5, None, f"{B, M, V, D} {lean}")
