@@ -255,6 +255,13 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
         for (int j = 0; j < 16; ++j)
           if (rel == 8 * (j >> 2) + (j & 3)) y[j] += o.g;
       }
+      // the last row again after the last: p g of a target may be past fp16 without that
+      const int left = a.nstream - ((s0 + s) * 64 + tile * 32) - 4 * h;
+      if (left + 4 * h < 32) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (8 * (j >> 2) + (j & 3) >= left) y[j] = 0.f;
+      }
     } else if (odd & (1 << tile)) {
 #pragma unroll
       for (int q = 0; q < 4; ++q) {

@@ -689,3 +689,15 @@ def test_fp16_gradients_of_few_positions(tk, B, M, V, D, entropy):
         g = rows((B, M), F32, 244) * torch.logspace(0, -4, M, device="cuda")
         h = rows((B, M), F32, 245, 0.2) if entropy else None
         check_grads(tk, Y, W, t, g, h, 2.0 / D ** 0.5, None, f"{B, M, V, D} {lean}")
+
+
+@pytest.mark.parametrize("D", [1, 64, 200, 300])
+@pytest.mark.parametrize("V", [1, 2, 33, 65])
+def test_fp16_gradients_where_the_last_token_has_all_the_probability(tk, D, V):
+    M = 5
+    X, W = rows((1, M, D), F16, 251), rows((1, V, D), F16, 252, 0.1)
+    X[0, :, 0], W[0, V - 1, 0] = 4.0, 4.0
+    t = torch.full((1, M), V - 1, dtype=torch.int32, device="cuda")
+    for h in (None, rows((1, M), F32, 254)):
+        check_grads(tk, X, W, t, rows((1, M), F32, 253), h, 1.0, None, f"{V, D}")
+        check_grads(tk, X, W, t - 1, rows((1, M), F32, 253), h, 1.0, None, f"{V, D} another")
