@@ -109,7 +109,8 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
  * used at all (it may hold anything) and gets dX 0.  Forbidden tokens get dW 0.
  * The two products take dz, X and W in fp16, each brought to fp16's range by powers
  * of two (dz over each position's own, X and W over their largest value's), sum in
- * fp32 in a fixed order and round once.
+ * fp32 in a fixed order and round once.  A dz below 3e-8 of its position's larger
+ * gradient has fewer than fp16's 11 bits; below 1.5e-11 of it, it is 0.
  * Workspace: tokens_logprobs_grad_workspace_bytes.
  */
 size_t tokens_logprobs_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int xdtype);

@@ -95,8 +95,8 @@ def grads(X, W, target, g, h=None, scale=1.0, bias=None):
     mag = (g.abs() + h.abs() * (1 + logp.clamp(min=-100).abs() + ent)) * p
     e = torch.where(keep, dp * (mag + h.abs() * p) + half(dt) * (dz.abs() + dp * mag), 0.0)
     gs = torch.where(active, torch.maximum(g.abs(), h.abs()), 0.0) * 2
-    if dt == torch.float16:  # the smallest step of the stored dz, and of X scaled by gs
-        e = torch.where(keep, e + gs * 2.0 ** -25 / 2048, 0.0)
+    # dz is stored in fp16 for either type, over gs and 2048 times larger: half its smallest step
+    e = torch.where(keep, e + gs * 2.0 ** -25 / 2048, 0.0)
     Xd = torch.where(active, X.double(), 0.0)
     Wd = W.double()
     if bias is not None:
