@@ -1725,8 +1725,9 @@ hipError_t launch_reduce(OutArgs& p, OutArgs& q, int64_t nb, hipStream_t s) {
 }
 
 // Both products over nb instances: p's and q's contractions in `sp` and `sq` shares.
+// `hold`: p's shares are joined later.
 template <int DT>
-hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, hipStream_t s) {
+hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, bool hold, hipStream_t s) {
   auto plan = [&](OutArgs& a, int splits) {
     const int nst = (a.chunks + 7) / 8;
     a.per = (nst + splits - 1) / splits;
@@ -1739,7 +1740,9 @@ hipError_t launch_out(OutArgs& p, int sp, OutArgs& q, int sq, int64_t nb, hipStr
   const dim3 grid((unsigned)(np + nq));
   out_kernel<DT><<<grid, NT_T, 0, s>>>(p, q, (int)np);
   const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_reduce<DT>(p, q, nb, s);
+  if (e != hipSuccess) return e;
+  OutArgs none{};
+  return launch_reduce<DT>(hold ? none : p, q, nb, s);
 }
 
 template <int DT, int DD>
@@ -1851,6 +1854,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
     const RowGrad* rg = w.rows + b0 * a.M;
     float4* scales = w.scales + b0;
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
+    int64_t shares = 0;  // of dX over the blocks of table rows
     for (int64_t v0 = 0; v0 < a.V; v0 += w.Vc) {
       const int64_t nv = std::min(w.Vc, a.V - v0), vp = (nv + 63) / 64 * 64, lv = grad_ld(vp);
       const CopyJob jx{(const uint16_t*)X + b0 * a.M * w.Dk, a.M, 0, a.M, w.Mp, lm, rg, nullptr,
@@ -1919,8 +1923,8 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       x.chunks = (int)(vp / 8);
       x.rows = rg;
       x.out = (uint16_t*)a.dX + b0 * a.M * a.D;
-      x.mode = !whole ? (v0 ? OUT_ADD : OUT_FIRST) : w.sx > 1 ? OUT_PART : OUT_16;
-      x.f32 = whole ? w.part : w.accx;
+      x.mode = w.sx > 1 ? OUT_PART : whole ? OUT_16 : v0 ? OUT_ADD : OUT_FIRST;
+      x.f32 = whole ? w.part : w.accx + shares * a.M * w.Dk;
       // dW: the block's table rows by D, over the positions
       q.At = (const char*)w.xt;
       q.Br = (const char*)w.dzt;
@@ -1932,15 +1936,16 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.chunks = (int)(w.Mp / 8);
       q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
       q.mode = w.sw > 1 ? OUT_PART : OUT_16;
-      q.f32 = w.part + (x.mode == OUT_PART ? nb * w.sx * a.M * w.Dk : 0);
-      if ((e = launch_out<DT>(x, whole ? w.sx : 1, q, w.sw, nb, s)) != hipSuccess) return e;
+      q.f32 = w.part + (whole && w.sx > 1 ? nb * w.sx * a.M * w.Dk : 0);
+      if ((e = launch_out<DT>(x, w.sx, q, w.sw, nb, !whole, s)) != hipSuccess) return e;
+      shares += w.sx > 1 ? x.splits : 0;
     }
     if (w.Vc < a.V) {  // dX from its fp32 sums
       OutArgs x{}, none{};
       x.D = (int)a.D;
       x.ldf = (int)w.Dk;
       x.R = x.os = a.M;
-      x.splits = 1;
+      x.splits = (int)std::max<int64_t>(1, shares);
       x.mode = OUT_PART;
       x.factor = a.scale / DZ_UP;
       x.rows = rg;

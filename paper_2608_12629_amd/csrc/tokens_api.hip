@@ -123,6 +123,10 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   } else {
     w.sx = out_splits(w.nb * cdiv(M, LP_BB) * dt, w.Vp / LP_DC);
     w.sw = out_splits(w.nb * cdiv(w.Vc, LP_BB) * dt, w.Mp / LP_DC);
+    // shares of every block of table rows are kept until the last (4,096 x 131,072 x 512
+    // in two blocks: 4,357 us with one share of each, 2,194 so)
+    if (w.Vc < V)
+      w.sx = (int)std::min<int64_t>(w.sx, std::max<int64_t>(1, LP_ACC_BYTES / (cdiv(V, w.Vc) * M * w.Dk * 4)));
   }
   take(w.xpad, w.Dk != D ? (size_t)(B * M * w.Dk) * 2 : 0);
   take(w.wpad, w.Dk != D ? (size_t)(B * V * w.Dk) * 2 : 0);
@@ -139,7 +143,7 @@ GradWs grad_carve(void* base, int64_t B, int64_t M, int64_t V, int64_t D) {
   take(w.dzt, held);
   take(w.xt, (size_t)(B * D * (w.Mp + 64)) * 2);
   take(w.wt, (size_t)(B * D * (Vall + 64)) * 2);
-  take(w.accx, w.Vc < V ? (size_t)(M * w.Dk) * 4 : 0);
+  take(w.accx, w.Vc < V ? (size_t)std::max(M * w.Dk * 4, LP_ACC_BYTES) : 0);
   const double cap = (double)OUT_WGS * LP_BB * 256;  // elements of all shared-out tiles
   const double px = Vall / 512 < 2 ? 0 : std::min((double)B * M * w.Dk * (Vall / 512), cap);
   const double pw = w.Mp / 512 < 2 ? 0 : std::min((double)B * V * w.Dk * (w.Mp / 512), cap);

@@ -151,6 +151,7 @@ struct LogprobsArgs {
 // fits LP_DZ_BYTES with its transpose) and instances (all or one) is stored in fp16,
 // and both products read it and transposed fp16 copies of X and W.
 constexpr int64_t LP_DZ_BYTES = (int64_t)1 << 30;
+constexpr int64_t LP_ACC_BYTES = (int64_t)1 << 30;
 constexpr int64_t LP_NARROW = 256, LP_NARROW_SCORES = 1 << 25;
 constexpr int64_t LP_EXACT = 64;     // fp16 positions up to which a target's dz is exact
 constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
@@ -173,7 +174,8 @@ struct GradWs {
   float4* scales;   // [B] the largest gs, the factors of X and W
   void *dz, *dzt;   // [nb, M, grad_ld(Vp)], [nb, Vp, grad_ld(Mp)]
   void *xt, *wt;    // [nb, D, grad_ld(Mp)], [nb, D, grad_ld(Vp)]
-  float* accx;      // [M, D] dX over the blocks of table rows, where there are several
+  float* accx;      // dX over the blocks of table rows, where there are several: [M, Dk],
+                    // or all their shares
   float* part;      // [nb, splits, rows, D] shares of a contraction
   int64_t Dk, Mp, Vp, Vc;
   bool narrow;      // short rows: dz is not stored (logprobs_narrow.h)

@@ -701,3 +701,10 @@ def test_fp16_gradients_where_the_last_token_has_all_the_probability(tk, D, V):
     for h in (None, rows((1, M), F32, 254)):
         check_grads(tk, X, W, t, rows((1, M), F32, 253), h, 1.0, None, f"{V, D}")
         check_grads(tk, X, W, t - 1, rows((1, M), F32, 253), h, 1.0, None, f"{V, D} another")
+
+
+def test_blocks_of_table_rows_of_many_results(tk):
+    """Several blocks of table rows and so many results of dX that each block adds to them."""
+    M, V, D = 9_000, 32_000, 2_304
+    X, W, t = rows((1, M, D), BF, 261), rows((1, V, D), BF, 262), ids(1, M, V, 263)
+    check_grads(tk, X, W, t, rows((1, M), F32, 264), None, 0.02, None, f"{M, V, D}")
