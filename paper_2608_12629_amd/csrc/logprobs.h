@@ -1149,10 +1149,10 @@ __device__ __forceinline__ float4 grad_scales(const float4* stats, int n, float4
 }
 
 // Transposed fp16 copies: in [nb, R, ld] rows r0 .. r0 + nr - 1 of each instance, times a
-// factor, -> out [nb, C, ldo] (C of their ld elements), zeros up to np.  Rows that take no part become zeros: of X
-// those without a gradient (the others times gs over the largest too), of W the forbidden
-// tokens.  64 x 64 values at a time: a thread reads 8 columns of two rows and stores them
-// in LDS as pairs of rows, and writes 8 rows of two columns.
+// factor, -> out [nb, C, ldo] (C of their ld elements), zeros up to np.  Rows that take no
+// part become zeros: of X those without a gradient (the others times gs over the largest
+// too), of W the forbidden tokens.  64 x 64 values at a time: a thread reads 8 columns of
+// two rows and stores them in LDS as pairs of rows, and writes 8 rows of two columns.
 struct CopyJob {
   const uint16_t* in;
   int64_t R, r0, nr, np, ldo;
@@ -1709,8 +1709,8 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
 template <int DT>
 hipError_t launch_reduce(OutArgs& p, OutArgs& q, int64_t nb, hipStream_t s) {
   // more threads to a result while there are few results: many shares of few rows would
-  // be as many latencies one after another (one position, 131,072 x 1,024:
-  // the call 519 -> 460 us)
+  // be as many latencies one after another (one position, 131,072 x 1,024: the call
+  // 519 -> 460 us)
   auto blocks = [&](OutArgs& a) -> int64_t {
     if (a.mode != OUT_PART) return 0;
     const int64_t n = nb * a.R * ((a.D + 7) / 8);

@@ -3,9 +3,8 @@
 // turns it into dz in registers and multiplies that on, once with the positions as its
 // own rows (dX) and once with the table rows (dW).  Four products instead of three, but
 // none of the 8 bytes a score that writing and reading dz twice costs, which bound rows
-// this short: 16,384 x 16,384 bf16 of 64 / 128 / 256 elements 627 / 703 / 848 ->
-// 209 / 332 / 672 us, 8 x 4,096 x
-// 1,024 x 128 104 -> 74 us.
+// this short: 16,384 x 16,384 bf16 of 64 / 128 / 256 elements 627 / 703 / 848 -> 209 /
+// 332 / 672 us, 8 x 4,096 x 1,024 x 128 104 -> 74 us.
 //
 // A wave owns 32 rows, which stay in registers as the columns (B) of 32 x 32 x 16 MFMAs;
 // the other side's rows stream through LDS in stages of 64.  Per tile of 32:

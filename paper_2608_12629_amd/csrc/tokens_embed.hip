@@ -451,7 +451,7 @@ constexpr int PAD_CHUNKS = 2048;  // of a workgroup
 
 // A thread makes 16-byte chunks of the copy of 32-bit words, which start wherever a row
 // does; the workgroups past the first nx are w's.  Bound by HBM: 43,047 rows of 1,331
-// elements 43 us (5.3 TB/s read and written; a workgroup per row or so: 185).
+// elements 43 us (5.3 TB/s read and written; with 64 rows to a workgroup 185).
 __global__ __launch_bounds__(256) void pad_kernel(PadJob x, PadJob w, int D, int ch, int64_t nx) {
   const bool is_x = (int64_t)blockIdx.x < nx;
   const PadJob j = is_x ? x : w;
