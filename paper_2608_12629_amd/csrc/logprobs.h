@@ -713,6 +713,7 @@ struct FinishArgs {
   const int32_t* target;
   int64_t rows, ts, ldz, groups;
   int splits, V, k;
+  bool all;                        // every score is stored, not those that a bound keeps
   float *logprob, *entropy, *lse;  // of this block of rows; ts positions an instance
   int32_t* top_idx;
   float* top_logprob;
@@ -803,8 +804,8 @@ __global__ __launch_bounds__(256) void finish_top_kernel(FinishArgs a) {
       ti[j] = have ? v : -1;
       tl[j] = have ? (key_score(key) - st.m) - logs : NEG_INF;
     };
-    // with few groups (a table of up to 4,096 rows) the entries themselves
-    const bool direct = G <= TOP_GROUPS;
+    // with few groups (a table of up to 4,096 rows) the entries themselves, if all are stored
+    const bool direct = a.all && G <= TOP_GROUPS;
     uint32_t mine = 0;
     const float* src = direct ? zr : gm;
     const int nsrc = direct ? a.V : G;
@@ -1690,6 +1691,7 @@ hipError_t launch_logprobs_dt(const LogprobsArgs& a, const LogprobsWs& w, hipStr
     f.splits = w.plan.head_splits + w.plan.splits;
     f.V = (int)a.V;
     f.k = a.k;
+    f.all = w.plan.head == 0;
     f.logprob = a.logprob + m0;
     f.entropy = a.entropy ? a.entropy + m0 : nullptr;
     f.lse = a.lse + m0;
