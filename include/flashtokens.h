@@ -82,8 +82,8 @@ int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, 
  * has lse and logprob -inf and entropy 0.  xdtype bf16 or fp16 (fp32 is
  * FKM_ERR_UNSUPPORTED).  A row of X with a NaN has NaN results and no other
  * row has; its top_idx are valid or -1.  D that is no multiple of 8 runs on padded
- * copies.  scale must be finite.  Scores that overflow fp32 are outside the
- * contract.
+ * copies.  scale must be finite.  Products scale * <x, w> of magnitude 2^127 and
+ * more are outside the contract; offsets may have any value but NaN and +inf.
  * Workspace: tokens_logprobs_workspace_bytes.
  */
 size_t tokens_logprobs_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int k,
@@ -95,7 +95,9 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
 
 /*
  * The gradient of sum_m g_m logprob_m + h_m entropy_m in X and W (bias is a
- * constant).  The scores are computed again; with p = exp(z - lse),
+ * constant).  The scores are computed again; with p = exp(z - lse) (with offsets, a
+ * row whose |lse| is 4,096 or more has its own maximum and sum taken again, as
+ * fp32 holds neither p nor the number of tokens in such an lse),
  *   dz = g (1[v = target] - p) - h p (z - lse + entropy)
  *   dX = scale * dz W,   dW = scale * dz^T X.
  *   lse       [B, M] fp32  of tokens_logprobs (read)

@@ -977,11 +977,51 @@ __device__ __forceinline__ float dot_chunk(const uint4& x, const uint4& y, float
 // into dW (the same: 2.2e-4, 2.1e-4 being the results' own rounding).
 constexpr float DZ_UP = 2048.f;
 
+// fp32 holds an lse far from 0 to half a step only: from FAR on, where that is 2^-12 and
+// more of p (an offset of -2^20 that all of a row's tokens share: 3%; of the type's lowest
+// value: p = 1 for each of them), a row's maximum and sum are taken again and kept apart.
+constexpr float FAR = 4096.f;
+
+// Both of one row by a workgroup of 512 threads, eight to a table row.  sh: 8 values.
+template <int DT>
+__device__ __forceinline__ Stat far_stat(const uint16_t* x, const uint16_t* W, const float* bias,
+                                         float scale, int V, int D, Stat* sh) {
+  const int tid = threadIdx.x, l = tid & 7;
+  Stat st = stat_none();
+  for (int v0 = 0; v0 < V; v0 += 64) {
+    const int v = v0 + (tid >> 3);
+    const float bz = v < V ? bias[v] : NEG_INF;
+    float z = 0.f;
+    if (bz != NEG_INF) {
+      const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)v * D);
+#pragma unroll 4
+      for (int c = l; c < D / 8; c += 8) z = dot_chunk<DT>(reinterpret_cast<const uint4*>(x)[c], w[c], z);
+    }
+#pragma unroll
+    for (int m = 1; m < 8; m <<= 1) z += __shfl_xor(z, m);
+    if (bz == NEG_INF) continue;
+    z = __builtin_fmaf(z, scale, bz);
+    if (z > st.m) stat_raise(st, z);
+    st.s += __builtin_amdgcn_exp2f((z - st.m) * LOG2E);
+  }
+#pragma unroll
+  for (int m = 8; m < 64; m <<= 1) {
+    const Stat o = {__shfl_xor(st.m, m), __shfl_xor(st.s, m), 0.f};
+    st = stat_merge(tid & m ? o : st, tid & m ? st : o);
+  }
+  __syncthreads();
+  if ((tid & 63) == 0) sh[tid >> 6] = st;
+  __syncthreads();
+  st = sh[0];
+  for (int i = 1; i < 8; ++i) st = stat_merge(st, sh[i]);
+  return st;
+}
+
 // What each position's gradient needs, and the largest gs and magnitudes: X's of the
 // rows that take part, W's of the tokens that do.  A workgroup goes over blocks of `rb`
 // rows (about 64 KiB) of X, or past the first `nx` workgroups of W: first a thread per
 // row, then all threads through the rows' 16-byte chunks.
-template <int DT>
+template <int DT, bool BIAS>
 __global__ __launch_bounds__(512) void grad_rows_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
     const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
@@ -990,6 +1030,8 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
   __shared__ float sh[8][2];
   __shared__ bool part[512];
   __shared__ float zt_s[DT == DT_F16 ? 512 : 1];
+  __shared__ float lse_s[BIAS ? 512 : 1], more_s[BIAS ? 512 : 1];
+  __shared__ Stat far_s[8];
   const int64_t b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const bool is_x = (int)blockIdx.x < nx;
@@ -1004,6 +1046,25 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
   };
   for (int64_t r0 = (is_x ? blockIdx.x : blockIdx.x - nx) * (int64_t)rb; r0 < rows; r0 += nblk * rb) {
     const int nr = (int)min<int64_t>(rb, rows - r0);
+    if (BIAS && is_x) {
+      bool far = false;
+      if (tid < nr) {
+        const int64_t i = b * M + r0 + tid;
+        const float l = lse[i];
+        far = __builtin_fabsf(l) >= FAR && l != NEG_INF && (g[i] != 0.f || (h && h[i] != 0.f));
+        lse_s[tid] = l;
+        more_s[tid] = 0.f;
+        part[tid] = far;
+      }
+      if (__syncthreads_or(far)) {
+        for (int q = 0; q < nr; ++q) {
+          if (!part[q]) continue;
+          const Stat st = far_stat<DT>(in + (r0 + q) * D, W + b * V * D, bias + b * V, scale, V, D, far_s);
+          if (tid == 0) lse_s[q] = st.m, more_s[q] = log2f(st.s);
+        }
+        __syncthreads();
+      }
+    }
     if (DT == DT_F16 && exact) {
       if (is_x) {
         // the targets' scores: `lpr` lanes a row, four rows of each at a time
@@ -1042,24 +1103,24 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         RowGrad r;
         const int t = target[i];
         const bool ok = (unsigned)t < (unsigned)V;
-        r.target = ok && (!bias || bias[b * V + (ok ? t : 0)] != NEG_INF) ? t : -1;
-        r.lse = lse[i];
+        r.target = ok && (!BIAS || bias[b * V + (ok ? t : 0)] != NEG_INF) ? t : -1;
+        r.lse = BIAS ? lse_s[tid] : lse[i];
+        r.more = BIAS ? more_s[tid] : 0.f;
         r.g = r.target >= 0 ? g[i] : 0.f;
-        r.h = h ? h[i] : 0.f;
-        r.ent = h ? ent[i] : 0.f;
-        r.active = r.lse != NEG_INF && (r.g != 0.f || r.h != 0.f);
+        float rh = h ? h[i] : 0.f;
+        const float re = h ? ent[i] : 0.f;
+        r.active = r.lse != NEG_INF && (r.g != 0.f || rh != 0.f);
         r.gs = 1.f;
-        r.pad = 0;
-        const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(r.h));
+        const float big = __builtin_fmaxf(__builtin_fabsf(r.g), __builtin_fabsf(rh));
         float u = 0.f;  // dz of the target, where it is the row's largest
         if (DT == DT_F16 && exact) {
           if (r.active && r.target >= 0) {
-            const float z = zt_s[tid] + (bias ? bias[b * V + r.target] : 0.f);
-            const float lp = __builtin_fminf(z - r.lse, 0.f), p = __expf(lp);
-            if (r.h == 0.f) {
+            const float z = zt_s[tid] + (BIAS ? bias[b * V + r.target] : 0.f);
+            const float lp = __builtin_fminf((z - r.lse) - r.more * LN2, 0.f), p = __expf(lp);
+            if (rh == 0.f) {
               u = r.g * __builtin_fmaxf(1.f - p, 0x1p-8f);
             } else {
-              u = r.g * (1.f - p) - (p > 0.f ? r.h * p * (lp + r.ent) : 0.f);
+              u = r.g * (1.f - p) - (p > 0.f ? rh * p * (lp + re) : 0.f);
               if (__builtin_fabsf(u) < 0.25f * big) u = 0.f;
             }
             const float a = __builtin_fabsf(u);
@@ -1069,20 +1130,30 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         if (u != 0.f) {
           r.gs = u;
           r.g /= u;
-          r.h /= u;
+          rh /= u;
         } else if (r.active && big <= __FLT_MAX__) {
           int e;
           (void)frexpf(big, &e);
           e = min(max(e, -120), 120);
           r.gs = copysignf(ldexpf(1.f, e), r.g);
           r.g *= copysignf(ldexpf(1.f, -e), r.g);
-          r.h *= 1.f / r.gs;
+          rh *= 1.f / r.gs;
+        }
+        r.c0 = -DZ_UP * __builtin_fmaf(rh, re, r.g);
+        r.c1 = -DZ_UP * LN2 * rh;
+        r.g *= DZ_UP;
+        if (BIAS) {
+          const float f = __builtin_amdgcn_exp2f(-r.more);
+          r.c0 = f * __builtin_fmaf(-r.more, r.c1, r.c0);
+          r.c1 *= f;
+        } else {
+          r.lse *= LOG2E;
         }
         out[i] = r;
         part[tid] = r.active;
         if (r.active) gsmax = __builtin_fmaxf(gsmax, __builtin_fabsf(r.gs));
       } else {
-        part[tid] = !bias || bias[b * V + r0 + tid] != NEG_INF;
+        part[tid] = !BIAS || bias[b * V + r0 + tid] != NEG_INF;
       }
     }
     __syncthreads();
@@ -1229,15 +1300,13 @@ struct DzArgs {
 };
 
 // dz of 256 positions by a share of the column blocks, in fp16, and its transpose.  The
-// scores come as in score_kernel; with the row's constants c0 = -(h entropy + g) and c1 =
-// -h ln 2 (times DZ_UP), dz = 2^l (c0 + c1 l), l = log2 p one fma of the accumulator, and g
-// more at the target.  32 x 64 values at a time go through the wave's part of the
+// scores come as in score_kernel.  32 x 64 values at a time go through the wave's part of the
 // finished stage's buffer, so that lines of both results are written whole.
 template <int DT, bool BIAS, bool ENT>
 __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   using Z = NtSize;
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
-  __shared__ float4 row_s[LP_BB];  // c0, c1, lse in units of log 2, g
+  __shared__ float4 row_s[LP_BB];  // c0, c1, lse, g
   __shared__ int tgt_s[LP_BB];     // -1: none; -2: the row takes no part
   int sp, bb;
   int64_t b;
@@ -1259,8 +1328,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     RowGrad rg;
     rg.active = 0;
     if (in.b0 + r < a.M) rg = a.rows[b * a.M + in.b0 + r];
-    row_s[r] = make_float4(-DZ_UP * __builtin_fmaf(rg.h, rg.ent, rg.g), -DZ_UP * LN2 * rg.h,
-                           rg.lse * LOG2E, DZ_UP * rg.g);
+    row_s[r] = make_float4(rg.c0, rg.c1, rg.lse, rg.g);
     tgt_s[r] = rg.active ? rg.target : -2;
   }
   __syncthreads();
@@ -1301,7 +1369,7 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
             const float x = acc[tp][tc][4 * q + r];
             float l;
             if constexpr (BIAS)  // in natural units: an offset may be the type's lowest value
-              l = __builtin_fmaf(__builtin_fmaf(x, a.scale, bz[r]), LOG2E, -rc.z);
+              l = (__builtin_fmaf(x, a.scale, bz[r]) - rc.z) * LOG2E;
             else
               l = __builtin_fmaf(x, c2, -rc.z);
             const float p = __builtin_amdgcn_exp2f(l);
@@ -1375,8 +1443,7 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
   RowGrad rg;
   rg.active = 0;
   if (m < a.M) rg = rows[b * a.M + m];
-  const float c0 = -DZ_UP * __builtin_fmaf(rg.h, rg.ent, rg.g), c1 = -DZ_UP * LN2 * rg.h;
-  const float lse2 = rg.lse * LOG2E, c2 = a.scale * LOG2E;
+  const float c2 = a.scale * LOG2E;
   uint32_t y2[VPT / 2];
 #pragma unroll
   for (int j = 0; j < VPT; j += 4) {
@@ -1391,12 +1458,12 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
       const float bz = BIAS && v < a.V ? a.bias[b * a.V + v] : 0.f;
       float l;
       if constexpr (BIAS)
-        l = __builtin_fmaf(__builtin_fmaf(x[r], a.scale, bz), LOG2E, -lse2);
+        l = (__builtin_fmaf(x[r], a.scale, bz) - rg.lse) * LOG2E;
       else
-        l = __builtin_fmaf(x[r], c2, -lse2);
+        l = __builtin_fmaf(x[r], c2, -rg.lse);
       const float p = __builtin_amdgcn_exp2f(l);
-      y[r] = ENT ? p * __builtin_fmaf(__builtin_fmaxf(l, -1e30f), c1, c0) : p * c0;
-      if (v == rg.target) y[r] += DZ_UP * rg.g;
+      y[r] = ENT ? p * __builtin_fmaf(__builtin_fmaxf(l, -1e30f), rg.c1, rg.c0) : p * rg.c0;
+      if (v == rg.target) y[r] += rg.g;
       if (!rg.active || v >= a.V || bz == NEG_INF) y[r] = 0.f;
     }
     y2[j / 2] = half2_bits(y[0], y[1]);
@@ -1847,7 +1914,8 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   const int64_t rb = exact ? std::min(full, std::max<int64_t>(16, a.V / 256)) : full;
   const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
   const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
-  grad_rows_kernel<DT><<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
+  auto grad_rows = a.bias ? grad_rows_kernel<DT, true> : grad_rows_kernel<DT, false>;
+  grad_rows<<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
       (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias,
       a.scale, exact, a.M, (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;

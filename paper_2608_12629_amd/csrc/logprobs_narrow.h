@@ -49,8 +49,9 @@ struct NarrowArgs {
 template <int DT, int DD, bool IS_X, bool BIAS, bool ENT>
 __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* smem) {
   using Z = NarrowSize<DD>;
-  // per streamed row, three stages' worth (dX: the offset; dW: lz, c0, c1, g; see dz_of)
-  constexpr int NC = IS_X ? 1 : ENT ? 4 : 2;
+  // per streamed row, three stages' worth (dX: the offset; dW: lz, g, then c0, c1 or l0; see dz_of)
+  constexpr bool L0 = BIAS && !ENT;
+  constexpr int NC = IS_X ? 1 : ENT ? 4 : L0 ? 3 : 2;
   __shared__ __attribute__((aligned(16))) float con_s[3][NC][64];
   __shared__ __attribute__((aligned(16))) int tgt_s[3][64];
   __shared__ __attribute__((aligned(16))) uint16_t keep_s[3][64];  // all ones: takes part
@@ -107,18 +108,19 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   // for every load on its way)
   constexpr bool CON = !IS_X || BIAS;
   struct Con {
-    float lz, c0, c1, g;
+    float lz, l0, c0, c1, g;
     int t;
     bool keep;
   } con;
   auto row_con = [&](const RowGrad& r) {
-    con.lz = r.lse * LOG2E;
-    con.g = DZ_UP * r.g;
+    con.lz = r.lse;
+    con.g = r.g;
     if constexpr (ENT) {
-      con.c0 = -DZ_UP * __builtin_fmaf(r.h, r.ent, r.g);
-      con.c1 = -DZ_UP * LN2 * r.h;
+      con.c0 = r.c0;
+      con.c1 = r.c1;
     } else {
-      con.lz -= __builtin_log2f(con.g);
+      if constexpr (L0) con.l0 = __builtin_log2f(con.g) - r.more;
+      else con.lz -= __builtin_log2f(con.g);
       con.g = -con.g;
     }
     con.keep = r.active;
@@ -126,7 +128,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   };
   auto fetch_con = [&](int s) {
     const int i = (s0 + s) * 64 + tid;
-    con = {0, 0, 0, 0, -1, false};
+    con = {0, 0, 0, 0, 0, -1, false};
     if (!CON || tid >= 64 || i >= a.nstream) return;
     if constexpr (IS_X) {
       con.lz = a.bias[b * a.V + i];
@@ -145,6 +147,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
         con_s[k][2][tid] = con.c0;
         con_s[k][3][tid] = con.c1;
       }
+      if constexpr (L0) con_s[k][2][tid] = con.l0;
       tgt_s[k][tid] = con.t;
     }
     keep_s[k][tid] = con.keep ? 0xffff : 0;
@@ -168,7 +171,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   }
   float bz = 0.f;
   bool mine = false;  // the own row takes part
-  con = {0, 0, 0, 0, -1, false};
+  con = {0, 0, 0, 0, 0, -1, false};
   if (own < a.nown) {
     if constexpr (IS_X) {
       row_con(a.rows[b * a.M + own]);
@@ -218,23 +221,26 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   };
   // Scores of tile `tile` of stage s -> dz in fp32, DZ_UP times larger.  With gradients
   // of entropies as in dz_kernel; without, -dz = p g is one exponential (g >= 0, its
-  // sign is in gs): 2^(z - lz), lz the lse less log2 g.
+  // sign is in gs): 2^(z - lz), lz the lse less log2 g.  With offsets lz is the lse itself
+  // (see RowGrad), and l0 = log2 g - more.
   auto dz_of = [&](f32x16& x, int s, int tile) {
     const int k = s % 3, at = tile * 32 + 4 * h;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-      f32x4 f, f0, f1;
+      f32x4 f, f0, f1, fl;
       if constexpr (CON) f = *reinterpret_cast<const f32x4*>(&con_s[k][0][at + 8 * q]);
       if constexpr (!IS_X && ENT) {
         f0 = *reinterpret_cast<const f32x4*>(&con_s[k][2][at + 8 * q]);
         f1 = *reinterpret_cast<const f32x4*>(&con_s[k][3][at + 8 * q]);
       }
+      if constexpr (!IS_X && L0) fl = *reinterpret_cast<const f32x4*>(&con_s[k][2][at + 8 * q]);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float z = x[4 * q + r], lz = IS_X ? o.lz : f[r];
         float l;
         if constexpr (BIAS)  // in natural units: an offset may be the type's lowest value
-          l = __builtin_fmaf(__builtin_fmaf(z, a.scale, IS_X ? f[r] : bz), LOG2E, -lz);
+          l = __builtin_fmaf(__builtin_fmaf(z, a.scale, IS_X ? f[r] : bz) - lz, LOG2E,
+                             ENT ? 0.f : IS_X ? o.l0 : fl[r]);
         else
           l = __builtin_fmaf(z, c2, -lz);
         x[4 * q + r] = __builtin_amdgcn_exp2f(l);

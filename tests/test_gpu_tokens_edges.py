@@ -38,3 +38,109 @@ def test_best_of_small_tables_with_many_scores(tk, B, M, V, k, dt):
             again = tk.tokens_logprobs(X, W, t, k=k, scale=scale, bias=bias,
                                        ws=torch.full_like(ws, 0x42))
             assert torch.equal(got[3], again[3]) and torch.equal(got[4], again[4])
+
+
+# ---- gradients ------------------------------------------------------------------------
+# What tokens_ref.grads allows, with less slack: dz rounds to fp16 for either storage type
+# (half a step, 2^-11, or half the smallest step 2^-24 of what is stored 2048 times larger
+# over the row's scale, which is at most 4 times the larger gradient), and the errors of
+# scores are given per token.
+U, H16 = 2.0 ** -24, 2.0 ** -11
+
+
+def sharp_grads(z, zerr, X, W, t, g, h, scale):
+    """dX, dW and their bounds from the scores z in 64 bits (-inf: forbidden), off by zerr."""
+    dt, (B, M, V) = X.dtype, z.shape
+    lse = torch.logsumexp(z, -1, keepdim=True)
+    logp = z - lse
+    p = torch.exp(logp)
+    plogp = torch.where(p > 0, p * logp, 0.0)
+    ent = -plogp.sum(-1, keepdim=True)
+    has = (t >= 0) & (t < V)
+    at = torch.where(has, t, 0).long().unsqueeze(-1)
+    has = has & (torch.gather(z, 2, at).squeeze(-1) > -INF)
+    g = torch.where(has, g.double(), 0.0).unsqueeze(-1)
+    h = torch.zeros_like(g) if h is None else h.double().unsqueeze(-1)
+    active = (g != 0) | (h != 0)
+    keep = active & (z > -INF)
+    hot = torch.zeros_like(z).scatter_(2, at, 1.0)
+    dz = torch.where(keep, g * (hot - p) - h * (plogp + p * ent), 0.0)
+    # p's error: of its score, of the lse (the row's largest), of exponentials and their sums
+    dp = 2 * zerr + 2 * torch.where(z > -INF, zerr, 0.0).amax(-1, keepdim=True) + (128 + V / 256) * 4 * U
+    mag = (g.abs() + h.abs() * (2 + logp.clamp(min=-100).abs() + ent)) * p
+    e = torch.where(keep, dp * mag + H16 * (dz.abs() + dp * mag), 0.0)
+    gs = torch.where(active, torch.maximum(g.abs(), h.abs()), 0.0) * 4
+    e = torch.where(keep, e + gs * 2.0 ** -25 / 2048, 0.0)
+    Xd = torch.where(active, X.double(), 0.0)
+    Wd = torch.where((z > -INF).any(1).unsqueeze(-1), W.double(), 0.0)
+    dzt, et = dz.transpose(1, 2).contiguous(), e.transpose(1, 2).contiguous()
+    dX, dW = torch.matmul(dz, Wd) * scale, torch.matmul(dzt, Xd) * scale
+    eX = torch.matmul(e + V * U * (dz.abs() + e), Wd.abs()) * abs(scale)
+    eW = torch.matmul(et + M * U * (dzt.abs() + et), Xd.abs()) * abs(scale)
+    # the copies of W and X below 2^-28 of the largest (X's times their rows' scales)
+    eX += dz.abs().sum(-1, keepdim=True) * Wd.abs().amax((1, 2), keepdim=True) * 2.0 ** -38 * abs(scale)
+    per = torch.where(gs > 0, dz.abs() / gs.clamp(min=1e-300), 0.0).sum(1).unsqueeze(-1)
+    eW += per * gs.amax(1, keepdim=True) * Xd.abs().amax((1, 2), keepdim=True) * 2.0 ** -38 * abs(scale)
+    if dt == F16 and B * M <= 64:  # X times a row's scale, no power of two here
+        eW += H16 * torch.matmul(dzt.abs() + et, Xd.abs()) * abs(scale)
+    tiny = torch.finfo(dt).smallest_normal * ref.half(dt) * 2
+    eX = eX + ref.half(dt) * (dX.abs() + eX) + tiny
+    eW = eW + ref.half(dt) * (dW.abs() + eW) + tiny
+    return dX, dW, eX, eW
+
+
+def check_sharp(tk, X, W, t, g, h, scale, bias, z, zerr, what):
+    _, ent, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=scale, bias=bias)
+    got = tk.tokens_logprobs_grad(X, W, t, lse, g, entropy=ent if h is not None else None, grad_entropy=h,
+                                  scale=scale, bias=bias)
+    wX, wW, eX, eW = sharp_grads(z, zerr, X, W, t, g, h, scale)
+    for a, want, bound, n in ((got[0], wX, eX, "dX"), (got[1], wW, eW, "dW")):
+        within(a, want, bound, f"{n} {what}")
+        # nothing written, or a twentieth of it left out, would show
+        assert not (want.abs().amax() > 0) or (bound.norm() < 0.05 * want.norm()), f"{n} {what}: a loose bound"
+    return got
+
+
+def half_rows(shape, dt, seed):
+    """Halves: products are quarters."""
+    return (rows(shape, F32, seed).round() / 2).to(dt)
+
+
+@pytest.mark.parametrize("M,V,D", [(300, 700, 64), (40, 500, 128), (500, 600, 250), (60, 700, 300),
+                                   (200, 500, 320), (3_000, 4_500, 264)])
+@pytest.mark.parametrize("dt", [BF, F16])
+def test_gradients_under_offsets_that_all_tokens_share(tk, M, V, D, dt):
+    """Offsets of the type's lowest value on every token (all alike) or on the only allowed
+    one, and of -2^20: the lse does not hold the logarithm of the sum there."""
+    X, W, t = half_rows((3, M, D), dt, 401), half_rows((3, V, D), dt, 402), ids(3, M, V, 403)
+    g = rows((3, M), F32, 404)
+    bias = torch.full((3, V), -INF, device="cuda")
+    bias[0] = LOWEST
+    bias[1, V // 2] = LOWEST
+    t[1, ::2] = V // 2
+    bias[2, 3:] = -2.0 ** 20 - 100
+    z = ref.scores(X, W, 0.5, None)  # eighths, which stay eighths below 2^21
+    z[0] = 0
+    z[1], z[1, :, V // 2] = -INF, 0
+    z[2, :, :3] = -INF
+    for h in (None, rows((3, M), F32, 405, 0.3)):
+        _, dW = check_sharp(tk, X, W, t, g, h, 0.5, bias, z, torch.zeros_like(z),
+                            f"{M, V, D, dt} {h is not None}")
+        assert not dW[1, :V // 2].any() and not dW[1, V // 2 + 1:].any() and not dW[2, :3].any()
+
+
+def test_gradients_under_lowest_offsets_beside_others(tk):
+    """The lowest value on some tokens, 0 on the rest: the same gradients as forbidden ones."""
+    for M, V, D in ((300, 700, 64), (60, 700, 300), (3_000, 4_500, 264)):
+        X, W, t = rows((1, M, D), BF, 411), rows((1, V, D), BF, 412), ids(1, M, V, 413)
+        t[0, ::3] = 1
+        g, h = rows((1, M), F32, 414), rows((1, M), F32, 415, 0.3)
+        off = rows((1, V), F32, 416) > 0.3
+        off[:, 1] = False
+        scale = 1 / D ** 0.5
+        bias = torch.where(off, LOWEST, 0.0)
+        z = ref.scores(X, W, scale, None) + torch.where(off, -1e30, 0.0).double().unsqueeze(1)
+        mag = torch.matmul(X.double().abs(), W.double().abs().transpose(1, 2).contiguous()) * scale
+        g = torch.where(off[0, t[0].clamp(0, V - 1).long()], 0.0, g)  # (such a target's dz is g)
+        for e in (None, h):
+            check_sharp(tk, X, W, t, g, e, scale, bias, z, (D + 2) * U * mag, f"{M, V, D} {e is not None}")
