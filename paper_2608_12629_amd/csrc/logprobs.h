@@ -1505,6 +1505,7 @@ struct OutArgs {
   float factor;
   const RowGrad* rows;   // dX: times gs of the row, over W's factor
   const float4* scales;  // dW (rows NULL): times the largest gs, over X's factor
+  const float* bias;     // dW: offsets of its rows; NULL: none
   uint16_t* out;
   float* f32;          // part [nb, splits, R, ldf] or acc [R, ldf]
   Raster grid;         // instances: the shares of each
@@ -1518,7 +1519,8 @@ __device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b) {
   return a.rows ? a.factor / s.z : a.factor / s.y * s.x;
 }
 
-// Eight consecutive results of a row (those below D) from `v`.  Rows of fp32 sums are
+// Eight consecutive results of a row (those below D) from `v`; zeros for rows that take no
+// part, whose sums of zeros times a NaN of another row are none.  Rows of fp32 sums are
 // ldf (D's multiple of 8) elements apart.  16-bit rows of other widths begin at any
 // element: three aligned pairs and the two elements that are left (65 x 43,047 x 1,331:
 // one by one 372 -> 305 us).
@@ -1526,12 +1528,18 @@ template <int DT>
 __device__ __forceinline__ void out_store(const OutArgs& a, float f, int64_t b, int sp, int64_t r, int d,
                                           float (&v)[8]) {
   if (a.mode == OUT_16) {
-    if (a.rows) f *= a.rows[b * a.os + r].gs;
+    bool keep = true;
+    if (a.rows) {
+      f *= a.rows[b * a.os + r].gs;
+      keep = a.rows[b * a.os + r].active;
+    } else if (a.bias) {
+      keep = a.bias[b * a.os + r] != NEG_INF;
+    }
     const int64_t at = (b * a.os + r) * a.D + d;
     uint16_t* o = a.out + at;
     alignas(16) uint16_t x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = Elem<DT>::narrow(v[e] * f);
+    for (int e = 0; e < 8; ++e) x[e] = keep ? Elem<DT>::narrow(v[e] * f) : (uint16_t)0;
     if (a.D % 8 == 0) {
       *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(x);
     } else if (d + 8 <= a.D) {
@@ -1866,6 +1874,7 @@ hipError_t launch_narrow(const GradArgs& a, const GradWs& g, const char* X, cons
   };
   side(x, X, a.M, W, a.V, g.wt, lv, g.sx, a.dX, g.part);
   x.out.rows = g.rows;
+  w.out.bias = a.bias;
   side(w, W, a.V, X, a.M, g.xt, lm, g.sw, a.dW,
        g.part + (x.out.mode == OUT_PART ? a.B * g.sx * a.M * g.Dk : 0));
   const hipError_t e = a.D <= 64 ? launch_narrow_dd<DT, 64>(a, x, w, s)
@@ -2003,6 +2012,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
       q.bs = vp * q.ld;
       q.R = nv;
       q.os = a.V;
+      q.bias = bias ? bias + v0 : nullptr;
       q.chunks = (int)(w.Mp / 8);
       q.out = (uint16_t*)a.dW + (b0 * a.V + v0) * a.D;
       q.mode = w.sw > 1 ? OUT_PART : OUT_16;

@@ -144,3 +144,28 @@ def test_gradients_under_lowest_offsets_beside_others(tk):
         g = torch.where(off[0, t[0].clamp(0, V - 1).long()], 0.0, g)  # (such a target's dz is g)
         for e in (None, h):
             check_sharp(tk, X, W, t, g, e, scale, bias, z, (D + 2) * U * mag, f"{M, V, D} {e is not None}")
+
+
+@pytest.mark.parametrize("M,V,D", [(300, 700, 64), (500, 600, 250), (60, 700, 300), (60, 700, 299),
+                                   (3_000, 4_500, 264), (200, 5_000, 512)])
+def test_rows_that_take_no_part_beside_nan(tk, M, V, D):
+    """Idle positions get dX 0 whatever an allowed token's row holds, forbidden tokens dW 0
+    whatever an active position's row holds."""
+    for dt in (BF, F16):
+        X, W, t = rows((1, M, D), dt, 421), rows((1, V, D), dt, 422), ids(1, M, V, 423)
+        g = rows((1, M), F32, 424)
+        g[:, ::3] = 0
+        bias = torch.zeros((1, V), device="cuda")
+        bias[:, 5::7] = -INF
+        for b in (None, bias):
+            _, _, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.1, bias=b)
+            Y, Z = X.clone(), W.clone()
+            Z[0, 3, 1] = float("nan")
+            dX, _ = tk.tokens_logprobs_grad(X, Z, t, lse, g, scale=0.1, bias=b)
+            assert not dX[:, ::3].any() and dX[0, t[0] == 3].isnan().any(-1).sum() >= (g[0, t[0] == 3] != 0).sum()
+            Y[0, 1, 2] = float("nan")
+            g[0, 1], t[0, 1] = 1.0, 4
+            _, dW = tk.tokens_logprobs_grad(Y, W, t, lse, g, scale=0.1, bias=b)
+            assert dW[0, 4].isnan().any()
+            if b is not None:
+                assert not dW[:, 5::7].any()
