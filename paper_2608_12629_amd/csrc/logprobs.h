@@ -1522,8 +1522,8 @@ __device__ __forceinline__ float out_factor(const OutArgs& a, int64_t b) {
 // Eight consecutive results of a row (those below D) from `v`; zeros for rows that take no
 // part, whose sums of zeros times a NaN of another row are none.  Rows of fp32 sums are
 // ldf (D's multiple of 8) elements apart.  16-bit rows of other widths begin at any
-// element: three aligned pairs and the two elements that are left (65 x 43,047 x 1,331:
-// one by one 372 -> 305 us).
+// element (an instance's first one too): three aligned pairs and the two elements that
+// are left (65 x 43,047 x 1,331: one by one 372 -> 305 us).
 template <int DT>
 __device__ __forceinline__ void out_store(const OutArgs& a, float f, int64_t b, int sp, int64_t r, int d,
                                           float (&v)[8]) {
@@ -1535,15 +1535,14 @@ __device__ __forceinline__ void out_store(const OutArgs& a, float f, int64_t b, 
     } else if (a.bias) {
       keep = a.bias[b * a.os + r] != NEG_INF;
     }
-    const int64_t at = (b * a.os + r) * a.D + d;
-    uint16_t* o = a.out + at;
+    uint16_t* o = a.out + (b * a.os + r) * a.D + d;
     alignas(16) uint16_t x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = keep ? Elem<DT>::narrow(v[e] * f) : (uint16_t)0;
     if (a.D % 8 == 0) {
       *reinterpret_cast<uint4*>(o) = *reinterpret_cast<const uint4*>(x);
     } else if (d + 8 <= a.D) {
-      const bool odd = at & 1;
+      const bool odd = (uintptr_t)o & 2;
 #pragma unroll
       for (int e = 0; e < 3; ++e) {
         const uint32_t even2 = x[2 * e] | (uint32_t)x[2 * e + 1] << 16;

@@ -169,3 +169,18 @@ def test_rows_that_take_no_part_beside_nan(tk, M, V, D):
             assert dW[0, 4].isnan().any()
             if b is not None:
                 assert not dW[:, 5::7].any()
+
+
+def test_instances_and_blocks_that_start_on_odd_elements(tk):
+    """dz past what is stored at once: instances one by one, blocks of table rows, each
+    with odd sizes, so that every other one's results begin in the middle of a pair."""
+    for B, M, V, D in ((2, 12_001, 12_001, 257), (1, 9_001, 40_003, 259)):
+        X, W, t = rows((B, M, D), BF, 431), rows((B, V, D), BF, 432), ids(B, M, V, 433)
+        g = rows((B, M), F32, 434)
+        _, _, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=0.06)
+        dX, dW = tk.tokens_logprobs_grad(X, W, t, lse, g, scale=0.06)
+        for b in range(B):
+            i = slice(b, b + 1)
+            wX, wW, eX, eW = ref.grads(X[i], W[i], t[i], g[i], None, 0.06)
+            within(dX[i], wX, eX, f"dX {B, M, V, D} {b}")
+            within(dW[i], wW, eW, f"dW {B, M, V, D} {b}")
