@@ -12,7 +12,7 @@ from typing import Optional, Tuple
 
 import torch
 
-from .kmeans import _DTYPE, ERR_UNSUPPORTED, KMeansError, _check, _need, lib
+from .kmeans import _DTYPE, KMeansError, _check, _need, lib  # noqa: F401
 
 _i64, _i32, _vp, _sz, _f32 = (ctypes.c_int64, ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t,
                               ctypes.c_float)
@@ -67,10 +67,10 @@ def _rows(t: torch.Tensor, name: str) -> Tuple[int, int, int]:
     return tuple(t.shape) if n == 3 else (1, *t.shape)
 
 
-def _workspace(ws: Optional[torch.Tensor], need: int, where: str, like: torch.Tensor,
+def _workspace(ws: Optional[torch.Tensor], need: int, like: torch.Tensor,
                dev: int) -> Tuple[torch.Tensor, int]:
-    if need == 0:
-        raise KMeansError(ERR_UNSUPPORTED, where)
+    if need == 0:  # arguments that the call rejects, and says why
+        return like.new_empty(0, dtype=torch.uint8), 0
     if ws is None or ws.numel() < need:
         ws = torch.empty(need, dtype=torch.uint8, device=like.device)
     return ws, _in(ws, "ws", dev, torch.uint8)
@@ -118,8 +118,7 @@ def tokens_embed_grad(grad: torch.Tensor, idx: torch.Tensor, V: int, scale: floa
     elif out.dtype not in (grad.dtype, torch.float32):
         raise TypeError(f"out must be {grad.dtype} or float32, got {out.dtype}")
     o = _in(out, "out", dev, None, B * V * D)
-    ws, w = _workspace(ws, lib.tokens_embed_grad_workspace_bytes(B, M, V, D, dt), "tokens_embed_grad",
-                       grad, dev)
+    ws, w = _workspace(ws, lib.tokens_embed_grad_workspace_bytes(B, M, V, D, dt), grad, dev)
     _check(lib.tokens_embed_grad(G, dt, t, B, M, V, D, scale, int(accumulate), o, _DTYPE[out.dtype], w,
                                  ws.numel(), stream), "tokens_embed_grad")
     return out
@@ -173,8 +172,7 @@ def tokens_logprobs(X: torch.Tensor, W: torch.Tensor, target: Optional[torch.Ten
         tl = _in(top_logprob, "top_logprob", dev, f32, B * M * k)
     elif top_idx is not None or top_logprob is not None:
         raise ValueError("top_idx and top_logprob need k > 0")
-    ws, p = _workspace(ws, lib.tokens_logprobs_workspace_bytes(B, M, V, D, k, dt), "tokens_logprobs", X,
-                       dev)
+    ws, p = _workspace(ws, lib.tokens_logprobs_workspace_bytes(B, M, V, D, k, dt), X, dev)
     _check(lib.tokens_logprobs(x, w, dt, bz, t, B, M, V, D, scale, k, lp,
                                _in(entropy, "entropy", dev, f32, B * M),
                                _in(lse, "lse", dev, f32, B * M), ti, tl, p, ws.numel(), stream),
@@ -208,8 +206,7 @@ def tokens_logprobs_grad(X: torch.Tensor, W: torch.Tensor, target: torch.Tensor,
         dX = torch.empty((B, M, D), dtype=X.dtype, device=X.device)
     if dW is None:
         dW = torch.empty((B, V, D), dtype=X.dtype, device=X.device)
-    ws, p = _workspace(ws, lib.tokens_logprobs_grad_workspace_bytes(B, M, V, D, dt),
-                       "tokens_logprobs_grad", X, dev)
+    ws, p = _workspace(ws, lib.tokens_logprobs_grad_workspace_bytes(B, M, V, D, dt), X, dev)
     _check(lib.tokens_logprobs_grad(x, w, dt, bz, t, l, ent, g, h, B, M, V, D, scale,
                                     _in(dX, "dX", dev, X.dtype, B * M * D),
                                     _in(dW, "dW", dev, X.dtype, B * V * D), p, ws.numel(), stream),

@@ -184,3 +184,32 @@ def test_instances_and_blocks_that_start_on_odd_elements(tk):
             wX, wW, eX, eW = ref.grads(X[i], W[i], t[i], g[i], None, 0.06)
             within(dX[i], wX, eX, f"dX {B, M, V, D} {b}")
             within(dW[i], wW, eW, f"dW {B, M, V, D} {b}")
+
+
+# ---- refusals ---------------------------------------------------------------------------
+def test_refusals_say_what_is_wrong(tk):
+    """The library's own status: sizes and numbers that no call takes are invalid, those
+    beyond this build's limits unsupported."""
+    from paper_2608_12629_amd.kmeans import ERR_INVALID_ARG, ERR_UNSUPPORTED
+    X, W, t = rows((1, 10, 64), BF, 501), rows((1, 50, 64), BF, 502), ids(1, 10, 50, 503)
+    none, f = t[:, :0], torch.zeros((1, 10), device="cuda")
+    wide = torch.zeros((1, 1, 8_200), dtype=BF, device="cuda")
+
+    def status(want, call, *a, **kw):
+        with pytest.raises(tk.KMeansError) as e:
+            call(*a, **kw)
+        assert e.value.status == want, e.value
+
+    status(ERR_INVALID_ARG, tk.tokens_logprobs, X, W, t, k=-1)
+    status(ERR_INVALID_ARG, tk.tokens_logprobs, X, W, t, k=51)
+    status(ERR_UNSUPPORTED, tk.tokens_logprobs, X, W, t, k=33)
+    status(ERR_INVALID_ARG, tk.tokens_logprobs, X[:, :0], W, none)
+    status(ERR_INVALID_ARG, tk.tokens_logprobs, X, W[:, :0], t)
+    status(ERR_UNSUPPORTED, tk.tokens_logprobs, X.float(), W.float(), t)
+    status(ERR_UNSUPPORTED, tk.tokens_logprobs, wide, wide)
+    status(ERR_INVALID_ARG, tk.tokens_embed, W, none)
+    status(ERR_INVALID_ARG, tk.tokens_embed_grad, X[:, :0], none, 50)
+    status(ERR_INVALID_ARG, tk.tokens_embed_grad, X, t, 0)
+    status(ERR_UNSUPPORTED, tk.tokens_embed_grad, X, t, (1 << 20) + 1)
+    status(ERR_INVALID_ARG, tk.tokens_logprobs_grad, X[:, :0], W, none, f[:, :0], f[:, :0])
+    status(ERR_UNSUPPORTED, tk.tokens_logprobs_grad, X.float(), W.float(), t, f, f)
