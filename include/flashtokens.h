@@ -13,6 +13,8 @@
  *   instances of M positions.  Tokens are int32 and local to an instance.
  * - A position whose token lies outside [0, V) (kmeans_assign's -1, padding) has
  *   no token: a zero row, log probability 0, no gradient.
+ * - Tables and rows of elements are 16-byte aligned; arrays of one 4-byte value a
+ *   position or token (tokens, offsets, statistics, alternatives) start anywhere.
  * - Offsets are 64 bits wide: no array has a size limit of its own.  B up to
  *   65,535, M up to 2^24 (2^23 - 64 for tokens_logprobs_grad), V up to 2^20, D up
  *   to 8,192.

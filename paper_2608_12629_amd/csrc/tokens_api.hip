@@ -30,9 +30,15 @@ int check_grads(int64_t B, int64_t M, int64_t V, int64_t D, int dt) {
   const int rc = check_scores(B, M, V, D, 0, dt);
   return rc ? rc : M > TOK_MAX_GRAD_M ? FKM_ERR_UNSUPPORTED : FKM_OK;
 }
-int check_optional(std::initializer_list<const void*> ps) {
-  for (const void* p : ps)
-    if (!aligned16(p)) return FKM_ERR_INVALID_ARG;
+// Arrays of one 4-byte element a position or token, which the kernels read and write one at a
+// time, may start at any: ids + t of a sequence.
+bool aligned4(const void* p) { return ((uintptr_t)p & 3) == 0; }
+int check_elements(std::initializer_list<const void*> needed,
+                   std::initializer_list<const void*> optional = {}) {
+  for (const void* p : needed)
+    if (!p || !aligned4(p)) return FKM_ERR_INVALID_ARG;
+  for (const void* p : optional)
+    if (!aligned4(p)) return FKM_ERR_INVALID_ARG;
   return FKM_OK;
 }
 
@@ -167,7 +173,7 @@ extern "C" {
 int tokens_embed(const void* W, int dtype, const int32_t* idx, int64_t B, int64_t M, int64_t V,
                  int64_t D, float scale, void* out, void* stream) {
   int rc;
-  if ((rc = check_ptrs({W, idx, out}))) return rc;
+  if ((rc = check_ptrs({W, out})) || (rc = check_elements({idx}))) return rc;
   if ((rc = check_tokens(B, M, V, D, dtype))) return rc;
   if ((rc = check_device())) return rc;
   return hip_status(launch_embed(W, dtype, idx, B, M, V, D, scale, out, (hipStream_t)stream));
@@ -182,7 +188,7 @@ int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, 
                       int64_t V, int64_t D, float scale, int accumulate, void* dW, int wdtype,
                       void* ws, size_t ws_bytes, void* stream) {
   int rc;
-  if ((rc = check_ptrs({G, idx, dW}))) return rc;
+  if ((rc = check_ptrs({G, dW})) || (rc = check_elements({idx}))) return rc;
   if ((rc = check_tokens(B, M, V, D, gdtype))) return rc;
   if (wdtype != gdtype && wdtype != DT_F32) return FKM_ERR_INVALID_ARG;
   const EmbedGradWs w = embed_grad_carve(ws, B, M, V, D);
@@ -203,8 +209,8 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
                     int k, float* logprob, float* entropy, float* lse, int32_t* top_idx,
                     float* top_logprob, void* ws, size_t ws_bytes, void* stream) {
   int rc;
-  if ((rc = check_ptrs({X, W, lse}))) return rc;
-  if ((rc = check_optional({bias, target, logprob, entropy, top_idx, top_logprob}))) return rc;
+  if ((rc = check_ptrs({X, W}))) return rc;
+  if ((rc = check_elements({lse}, {bias, target, logprob, entropy, top_idx, top_logprob}))) return rc;
   if (target && !logprob) return FKM_ERR_INVALID_ARG;
   if (k > 0 && (!top_idx || !top_logprob)) return FKM_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
@@ -230,8 +236,8 @@ int tokens_logprobs_grad(const void* X, const void* W, int xdtype, const float* 
                          int64_t V, int64_t D, float scale, void* dX, void* dW, void* ws,
                          size_t ws_bytes, void* stream) {
   int rc;
-  if ((rc = check_ptrs({X, W, target, lse, grad_logprob, dX, dW}))) return rc;
-  if ((rc = check_optional({bias, entropy, grad_entropy}))) return rc;
+  if ((rc = check_ptrs({X, W, dX, dW}))) return rc;
+  if ((rc = check_elements({target, lse, grad_logprob}, {bias, entropy, grad_entropy}))) return rc;
   if (grad_entropy && !entropy) return FKM_ERR_INVALID_ARG;
   if (!std::isfinite(scale)) return FKM_ERR_INVALID_ARG;
   if ((rc = check_grads(B, M, V, D, xdtype))) return rc;

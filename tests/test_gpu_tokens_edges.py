@@ -213,3 +213,31 @@ def test_refusals_say_what_is_wrong(tk):
     status(ERR_UNSUPPORTED, tk.tokens_embed_grad, X, t, (1 << 20) + 1)
     status(ERR_INVALID_ARG, tk.tokens_logprobs_grad, X[:, :0], W, none, f[:, :0], f[:, :0])
     status(ERR_UNSUPPORTED, tk.tokens_logprobs_grad, X.float(), W.float(), t, f, f)
+
+
+@pytest.mark.parametrize("B,M,V,D", [(1, 1, 300, 64), (1, 999, 700, 64), (1, 9_001, 500, 40), (1, 300, 900, 320),
+                                     (2, 301, 4_001, 24)])
+def test_values_that_start_at_any_element(tk, B, M, V, D):
+    """Tokens, offsets, statistics and gradients one element into an allocation (the next
+    tokens of a sequence) give what copies of them give."""
+    def late(x):
+        y = torch.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+        assert y.data_ptr() % 16 == 4
+        return y.copy_(x)
+
+    X, W, t = grid_rows((B, M, D), BF, 511), grid_rows((B, V, D), BF, 512), ids(B, M, V, 513)
+    bias, g, h = rows((B, V), F32, 514), rows((B, M), F32, 515), rows((B, M), F32, 516)
+    assert torch.equal(tk.tokens_embed(W, late(t)), tk.tokens_embed(W, t))
+    assert torch.equal(tk.tokens_embed_grad(X, late(t), V), tk.tokens_embed_grad(X, t, V))
+    want = tk.tokens_logprobs(X, W, t, k=3, scale=0.125, bias=bias)
+    outs = dict(zip(("logprob", "entropy", "lse", "top_idx", "top_logprob"), (late(a) for a in want)))
+    for a in outs.values():
+        a.zero_()
+    got = tk.tokens_logprobs(X, W, late(t), k=3, scale=0.125, bias=late(bias), **outs)
+    for a, b, o in zip(got, want, outs.values()):
+        assert a is o and torch.equal(a, b)
+    _, ent, lse, _, _ = want
+    dX, dW = tk.tokens_logprobs_grad(X, W, t, lse, g, entropy=ent, grad_entropy=h, scale=0.125, bias=bias)
+    dX2, dW2 = tk.tokens_logprobs_grad(X, W, late(t), late(lse), late(g), entropy=late(ent), grad_entropy=late(h),
+                                       scale=0.125, bias=late(bias))
+    assert torch.equal(dX, dX2) and torch.equal(dW, dW2)
