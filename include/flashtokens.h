@@ -111,10 +111,15 @@ int tokens_logprobs(const void* X, const void* W, int xdtype, const float* bias,
  * A position without a token, or whose token is forbidden, has no gradient of
  * its log probability; a row with neither gradient, or with lse -inf, is not
  * used at all (it may hold anything) and gets dX 0.  Forbidden tokens get dW 0.
- * The two products take dz, X and W in fp16, each brought to fp16's range by powers
- * of two (dz over each position's own, X and W over their largest value's), sum in
- * fp32 in a fixed order and round once.  A dz below 3e-8 of its position's larger
- * gradient has fewer than fp16's 11 bits; below 1.5e-11 of it, it is 0.
+ * The two products take dz, X and W in fp16, sum in fp32 in a fixed order and round
+ * once.  X and W are brought to fp16's range by the power of two of their instance's
+ * largest value (half of 2^-39 of that is rounded off), dz by one of its
+ * position's larger gradient (calls of up to 64 fp16 positions: by the target's dz, no
+ * power of two).  bf16 results are as far off as their own rounding, fp16 ones up to
+ * twice that.  A dz below 3e-8 of its position's larger gradient has fewer than 11
+ * bits; below 1.5e-11 of it, it is 0.  In dW a position counts with fewer bits of small
+ * values (of X and of dz) if its larger gradient is below 2^-12 of the instance's
+ * largest, of all values below 2^-40, and not at all below 2^-54.
  * Workspace: tokens_logprobs_grad_workspace_bytes.
  */
 size_t tokens_logprobs_grad_workspace_bytes(int64_t B, int64_t M, int64_t V, int64_t D, int xdtype);

@@ -298,9 +298,12 @@ __device__ __forceinline__ bool raster_place(const Raster& r, int id, int& a, in
 // (by value: a conditional between array elements puts the array into memory)
 __device__ __forceinline__ float pick(bool c, float a, float b) { return c ? a : b; }
 
+typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t half2_bits(float a, float b) {
-  typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-  return __builtin_bit_cast(uint32_t, h2{(_Float16)a, (_Float16)b});  // to nearest even
+  return __builtin_bit_cast(uint32_t, half2_t{(_Float16)a, (_Float16)b});  // to nearest even
+}
+__device__ __forceinline__ uint32_t half2_mul(uint32_t a, uint32_t b) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(half2_t, a) * __builtin_bit_cast(half2_t, b));
 }
 
 // One workgroup: 256 rows of X by a share of the column blocks (all shares within one
@@ -966,9 +969,11 @@ __device__ __forceinline__ float dot_chunk(const uint4& x, const uint4& y, float
 // types: 11 significant bits against bf16's 8 make dz's rounding an eighth, below that
 // of the results (bf16 dz: dX and dW off by 2.4e-3 of their norm, 1.7e-3 being their own
 // rounding; fp16: 1.7e-3).  All three are kept in range: each row's dz is stored over gs
-// and DZ_UP times larger; X (times gs over the largest gs) and W times the power of two
-// that brings their largest value just below 2^14, where fp16 holds every bf16 or fp16
-// value down to 2^-28 of that exactly.  gs is a power of two at or above max(|g|, |h|).
+// and DZ_UP times larger; X and W times the power of two that brings their largest value
+// just below 2^15, where fp16 holds every bf16 or fp16 value down to 2^-29 of that
+// exactly.  gs is a power of two at or above max(|g|, |h|).  dW sums over rows of
+// different gs: X's copy is times gs over the largest gs, but for what dz's transpose
+// takes of that (faint_part).
 // dz's rounding is then, with fp16 results, as large as theirs, and one relative error of
 // a row wherever one dz, the target's, makes most of it: over many rows 1.4 times the
 // results' own rounding, over few up to 2.3 times (1 position, 8 x 8,931 x 586: 3.5e-4).
@@ -977,8 +982,19 @@ __device__ __forceinline__ float dot_chunk(const uint4& x, const uint4& y, float
 // into dW (the same: 2.2e-4, 2.1e-4 being the results' own rounding).
 constexpr float DZ_UP = 2048.f;
 
+// Of a row whose gs is 2^-k of the largest, the factor that dz's transpose takes: nothing
+// down to 2^-12, then half of the exponent up to 14, so that with the rest in X's copy
+// either stays in fp16's normal range down to 2^-40 (all of it in X's copy: to 2^-25 or so,
+// and at 2^-36 a third of the row's dW was left).
+__device__ __forceinline__ float faint_part(float gs, float top) {
+  int a, b;
+  (void)frexpf(top, &a);
+  (void)frexpf(gs, &b);
+  return ldexpf(1.f, -min(max((a - b - 12) / 2, 0), 14));
+}
+
 // fp32 holds an lse far from 0 to half a step only: from FAR on, where that is 2^-12 and
-// more of p (an offset of -2^20 that all of a row's tokens share: 3%; of the type's lowest
+// more of p (an offset of -2^20 that all of a row's tokens share: 6%; of the type's lowest
 // value: p = 1 for each of them), a row's maximum and sum are taken again and kept apart.
 constexpr float FAR = 4096.f;
 
@@ -1105,7 +1121,8 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         const bool ok = (unsigned)t < (unsigned)V;
         r.target = ok && (!BIAS || bias[b * V + (ok ? t : 0)] != NEG_INF) ? t : -1;
         r.lse = BIAS ? lse_s[tid] : lse[i];
-        r.more = BIAS ? more_s[tid] : 0.f;
+        const float more = BIAS ? more_s[tid] : 0.f;  // (see RowGrad)
+        r.part = 1.f;
         r.g = r.target >= 0 ? g[i] : 0.f;
         float rh = h ? h[i] : 0.f;
         const float re = h ? ent[i] : 0.f;
@@ -1116,7 +1133,7 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         if (DT == DT_F16 && exact) {
           if (r.active && r.target >= 0) {
             const float z = zt_s[tid] + (BIAS ? bias[b * V + r.target] : 0.f);
-            const float lp = __builtin_fminf((z - r.lse) - r.more * LN2, 0.f), p = __expf(lp);
+            const float lp = __builtin_fminf((z - r.lse) - more * LN2, 0.f), p = __expf(lp);
             if (rh == 0.f) {
               u = r.g * __builtin_fmaxf(1.f - p, 0x1p-8f);
             } else {
@@ -1143,8 +1160,8 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         r.c1 = -DZ_UP * LN2 * rh;
         r.g *= DZ_UP;
         if (BIAS) {
-          const float f = __builtin_amdgcn_exp2f(-r.more);
-          r.c0 = f * __builtin_fmaf(-r.more, r.c1, r.c0);
+          const float f = __builtin_amdgcn_exp2f(-more);
+          r.c0 = f * __builtin_fmaf(-more, r.c1, r.c0);
           r.c1 *= f;
         } else {
           r.lse *= LOG2E;
@@ -1195,12 +1212,12 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
   }
 }
 
-// The power of two that brings values of magnitude up to m below 2^14.
-__device__ __forceinline__ float up_to_2_14(float m) {
+// The power of two that brings values of magnitude up to m below 2^15.
+__device__ __forceinline__ float up_to_2_15(float m) {
   if (!(m > 0.f)) return 1.f;
   int e;
   (void)frexpf(m, &e);
-  return ldexpf(1.f, min(14 - e, 126));
+  return ldexpf(1.f, min(15 - e, 126));
 }
 // (largest gs, factor of X, factor of W) from n statistics, by 256 threads.
 __device__ __forceinline__ float4 grad_scales(const float4* stats, int n, float4* sh) {
@@ -1217,19 +1234,20 @@ __device__ __forceinline__ float4 grad_scales(const float4* stats, int n, float4
   if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = o;
   __syncthreads();
   for (int i = 0; i < 4; ++i) take(sh[i]);
-  return make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_14(o.y), up_to_2_14(o.z), 0.f);
+  return make_float4(o.x > 0.f ? o.x : 1.f, up_to_2_15(o.y), up_to_2_15(o.z), 0.f);
 }
 
 // Transposed fp16 copies: in [nb, R, ld] rows r0 .. r0 + nr - 1 of each instance, times a
 // factor, -> out [nb, C, ldo] (C of their ld elements), zeros up to np.  Rows that take no
 // part become zeros: of X those without a gradient (the others times gs over the largest
-// too), of W the forbidden tokens.  64 x 64 values at a time: a thread reads 8 columns of
-// two rows and stores them in LDS as pairs of rows, and writes 8 rows of two columns.
+// too, but for faint_part, which the rows' constants for dW get), of W the forbidden
+// tokens.  64 x 64 values at a time: a thread reads 8 columns of two rows and stores them
+// in LDS as pairs of rows, and writes 8 rows of two columns.
 struct CopyJob {
   const uint16_t* in;
   int64_t R, r0, nr, np, ldo;
-  const RowGrad* rows;  // of X
-  const float* bias;    // of W
+  RowGrad* rows;      // of X, whose `part` is set
+  const float* bias;  // of W
   uint16_t* out;
   int tiles;  // np / 64; 0: no such job
   bool mixed; // columns 16 t + 8 h + i hold rows 16 t + 8 (i / 4) + 4 h + i % 4
@@ -1256,8 +1274,16 @@ __global__ __launch_bounds__(256) void copy_kernel(CopyJob x, CopyJob w, int C, 
       float f = 0.f;
       if (r < j.nr) {
         const int64_t ri = b * j.R + j.r0 + r;
-        if (is_x) f = j.rows[ri].active ? j.rows[ri].gs / sc.x * sc.y : 0.f;
-        else f = j.bias && j.bias[ri] == NEG_INF ? 0.f : sc.z;
+        if (is_x) {
+          const float gs = j.rows[ri].gs, part = faint_part(gs, sc.x);
+          f = j.rows[ri].active ? gs / sc.x * sc.y / part : 0.f;
+          if (blockIdx.y == 0 && c8 == 0) {
+            j.rows[ri].g *= part;
+            j.rows[ri].c0 *= part;
+            j.rows[ri].c1 *= part;
+            j.rows[ri].part = part;
+          }
+        } else f = j.bias && j.bias[ri] == NEG_INF ? 0.f : sc.z;
       }
       alignas(16) uint16_t x8[8] = {0, 0, 0, 0, 0, 0, 0, 0};
       const int c = ct + 8 * c8;
@@ -1308,6 +1334,8 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
   __shared__ __attribute__((aligned(16))) char smem[Z::SMEM];
   __shared__ float4 row_s[LP_BB];  // c0, c1, lse, g
   __shared__ int tgt_s[LP_BB];     // -1: none; -2: the row takes no part
+  __shared__ __attribute__((aligned(16))) uint32_t part_s[LP_BB];  // `part` twice
+  __shared__ uint64_t faint_s[LP_BB / 64];  // the rows with one
   int sp, bb;
   int64_t b;
   if (!raster_place(a.grid, blockIdx.x, sp, bb, b)) return;
@@ -1328,8 +1356,12 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
     RowGrad rg;
     rg.active = 0;
     if (in.b0 + r < a.M) rg = a.rows[b * a.M + in.b0 + r];
-    row_s[r] = make_float4(rg.c0, rg.c1, rg.lse, rg.g);
     tgt_s[r] = rg.active ? rg.target : -2;
+    const float f = rg.active ? rg.part : 1.f, up = 1.f / f;
+    row_s[r] = make_float4(rg.c0 * up, rg.c1 * up, rg.lse, rg.g * up);
+    part_s[r] = half2_bits(f, f);
+    const uint64_t faint = __ballot(f != 1.f);
+    if ((r & 63) == 0) faint_s[r / 64] = faint;
   }
   __syncthreads();
   NtLoop<DT> loop;
@@ -1406,6 +1438,17 @@ __global__ __launch_bounds__(NT_T, 1) void dz_kernel(DzArgs a) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         x[i] = nt_at<uint32_t>(sq, at(16 * h + i, n >> 1) + (n & 1) * 4);
+      if (faint_s[wp * 2 + tp / 2]) {
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const uint4 f = *reinterpret_cast<const uint4*>(&part_s[wp * 128 + tp * 32 + 16 * h + i]);
+          x[i] = half2_mul(x[i], f.x);
+          x[i + 1] = half2_mul(x[i + 1], f.y);
+          x[i + 2] = half2_mul(x[i + 2], f.z);
+          x[i + 3] = half2_mul(x[i + 3], f.w);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       if (vb + 2 * n < a.Vp) {
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
@@ -1443,7 +1486,8 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
   RowGrad rg;
   rg.active = 0;
   if (m < a.M) rg = rows[b * a.M + m];
-  const float c2 = a.scale * LOG2E;
+  const float c2 = a.scale * LOG2E, fp = rg.active ? rg.part : 1.f;
+  const float c0 = rg.c0 / fp, c1 = rg.c1 / fp, g = rg.g / fp;
   uint32_t y2[VPT / 2];
 #pragma unroll
   for (int j = 0; j < VPT; j += 4) {
@@ -1462,8 +1506,8 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
       else
         l = __builtin_fmaf(x[r], c2, -rg.lse);
       const float p = __builtin_amdgcn_exp2f(l);
-      y[r] = ENT ? p * __builtin_fmaf(__builtin_fmaxf(l, -1e30f), rg.c1, rg.c0) : p * rg.c0;
-      if (v == rg.target) y[r] += rg.g;
+      y[r] = ENT ? p * __builtin_fmaf(__builtin_fmaxf(l, -1e30f), c1, c0) : p * c0;
+      if (v == rg.target) y[r] += g;
       if (!rg.active || v >= a.V || bz == NEG_INF) y[r] = 0.f;
     }
     y2[j / 2] = half2_bits(y[0], y[1]);
@@ -1474,6 +1518,8 @@ __global__ __launch_bounds__(256, CB <= 2 ? 3 : 2) void few_dz_kernel(
 #pragma unroll
     for (int j = 0; j < VPT / 2; j += 2) *reinterpret_cast<uint2*>(o + 2 * j) = make_uint2(y2[j], y2[j + 1]);
   }
+#pragma unroll
+  for (int j = 0; j < VPT / 2; ++j) y2[j] = half2_mul(y2[j], half2_bits(fp, fp));
   __syncthreads();
   uint16_t* tile = reinterpret_cast<uint16_t*>(&red[0][0]);
 #pragma unroll
@@ -1929,7 +1975,7 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);
-    const RowGrad* rg = w.rows + b0 * a.M;
+    RowGrad* rg = w.rows + b0 * a.M;
     float4* scales = w.scales + b0;
     const float* bias = a.bias ? a.bias + b0 * a.V : nullptr;
     int64_t shares = 0;  // of dX over the blocks of table rows

@@ -113,14 +113,16 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
     bool keep;
   } con;
   auto row_con = [&](const RowGrad& r) {
+    const float f = IS_X ? 1.f / r.part : 1.f;
     con.lz = r.lse;
-    con.g = r.g;
+    con.g = r.g * f;
     if constexpr (ENT) {
-      con.c0 = r.c0;
-      con.c1 = r.c1;
+      con.c0 = r.c0 * f;
+      con.c1 = r.c1 * f;
     } else {
-      if constexpr (L0) con.l0 = __builtin_log2f(con.g) - r.more;
-      else con.lz -= __builtin_log2f(con.g);
+      const float l0 = __builtin_log2f(-r.c0 * f);
+      if constexpr (L0) con.l0 = l0;
+      else con.lz -= l0;
       con.g = -con.g;
     }
     con.keep = r.active;
@@ -222,7 +224,7 @@ __device__ __forceinline__ void narrow_run(const NarrowArgs& a, int id, char* sm
   // Scores of tile `tile` of stage s -> dz in fp32, DZ_UP times larger.  With gradients
   // of entropies as in dz_kernel; without, -dz = p g is one exponential (g >= 0, its
   // sign is in gs): 2^(z - lz), lz the lse less log2 g.  With offsets lz is the lse itself
-  // (see RowGrad), and l0 = log2 g - more.
+  // (see RowGrad), and l0 = log2 g, less `more`.
   auto dz_of = [&](f32x16& x, int s, int tile) {
     const int k = s % 3, at = tile * 32 + 4 * h;
 #pragma unroll

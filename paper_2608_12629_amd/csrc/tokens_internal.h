@@ -157,17 +157,18 @@ constexpr int64_t LP_EXACT = 64;     // fp16 positions up to which a target's dz
 constexpr int64_t STATS_WGS = 1024;  // most workgroups of an instance's statistics
 // One position.  p = 2^l of a score z: without offsets l = z log2 e - lse, lse in units of
 // log 2, one fma of the accumulator; offsets (one may be the type's lowest value) need
-// l + more = (z - lse) log2 e, lse in natural units.  dz = 2^(l + more) (c0 + c1 (l + more)),
-// and g more at the target.
+// l + more = (z - lse) log2 e, lse in natural units and `more` 0 but for far rows.  dz =
+// 2^(l + more) (c0 + c1 (l + more)), and g more at the target.
 struct RowGrad {
   float g;        // gradient of the log probability over `gs` (>= 0 without gradients of
                   // entropies), DZ_UP times that
-  float c0, c1;   // -(h entropy + g) and -h ln 2 (both less `more`), h the entropy's gradient
+  float c0, c1;   // -(h entropy + g) and -h ln 2 (`more` in them), h the entropy's gradient
   float lse;
   int target;     // -1: none
   int active;     // takes part at all
   float gs;       // what g, h and so dz of this row are divided by
-  float more;     // 0 but for far rows
+  float part;     // what dW takes of gs over the largest into dz (faint_part): g, c0 and c1
+                  // are times this
 };
 // Elements from row to row of dz and the copies: 128 bytes past a multiple of 1 KiB, so
 // that a stage's 64 bytes of each of 512 rows do not all lie in one L2 channel.

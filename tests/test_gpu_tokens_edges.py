@@ -186,6 +186,38 @@ def test_instances_and_blocks_that_start_on_odd_elements(tk):
             within(dW[i], wW, eW, f"dW {B, M, V, D} {b}")
 
 
+@pytest.mark.parametrize("M,V,D", [(300, 700, 64), (500, 600, 250), (60, 700, 300), (3_000, 4_500, 264)])
+@pytest.mark.parametrize("down", [13, 24, 30, 40])
+def test_faint_positions_of_their_own_tokens(tk, M, V, D, down):
+    """Half of the positions have gradients 2^down times smaller, and tokens that the other
+    half gives no probability: those tokens' gradients are as precise as the others'."""
+    X, W = rows((1, M, D), BF, 441), rows((1, V, D), BF, 442)
+    faint = torch.arange(M, device="cuda") % 2 == 1
+    far = torch.arange(V, device="cuda") % 2 == 1
+    X[:, :, :2], W[:, :, :2] = 0, 0  # 400 apart: the products below add a few
+    X[0, faint, 0], X[0, ~faint, 1] = 20, 20
+    W[0, far, 0], W[0, ~far, 1] = 20, 20
+    t = torch.randint(0, V // 2, (1, M), device="cuda") * 2 + faint.int()
+    t = t.to(torch.int32)
+    g = rows((1, M), F32, 444).abs().clamp(min=0.25)
+    h = rows((1, M), F32, 445, 0.1)
+    small = torch.where(faint, 2.0 ** -down, 1.0)
+    scale = 1.0 if D <= 64 else 0.5
+    for ent in (False, True):
+        _, e, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=scale)
+        kw = dict(entropy=e, scale=scale) if ent else dict(scale=scale)
+        even = tk.tokens_logprobs_grad(X, W, t, lse, g, grad_entropy=h if ent else None, **kw)
+        got = tk.tokens_logprobs_grad(X, W, t, lse, g * small, grad_entropy=h * small if ent else None, **kw)
+        # the same numbers times a power of two, but for what the copies of X and dz round
+        # off their smaller values (at most half a step, 2^-11 of a product) and the
+        # results' own rounding, half a step of bf16 (2^-8) on both sides
+        for a, b, part in ((got[0], even[0], faint), (got[1], even[1], far)):
+            x, y = a[0, part].double() * 2.0 ** down, b[0, part].double()
+            assert (x - y).norm() <= 2.0 ** -8 * y.norm(), ((x - y).norm() / y.norm()).item()
+            assert (x - y).abs().amax() <= 2.0 ** -7 * y.abs().amax()
+            assert torch.equal(a[0, ~part], b[0, ~part])
+
+
 # ---- refusals ---------------------------------------------------------------------------
 def test_refusals_say_what_is_wrong(tk):
     """The library's own status: sizes and numbers that no call takes are invalid, those
