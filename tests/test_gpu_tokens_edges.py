@@ -218,6 +218,63 @@ def test_faint_positions_of_their_own_tokens(tk, M, V, D, down):
             assert torch.equal(a[0, ~part], b[0, ~part])
 
 
+@pytest.mark.parametrize("M,V,D", [(5_000, 700, 64), (5_000, 700, 200), (40, 3_000, 300), (3_000, 4_500, 264)])
+@pytest.mark.parametrize("entropy", [False, True])
+def test_bf16_gradients_take_dz_in_11_bits(tk, M, V, D, entropy):
+    """How many results are not the rounding of the exact ones.  A dz that is off by up to
+    2^-11 (2^-12 in the mean) moves a result by no more than that, relative to the root of
+    its products' squares, and a result of at least that size (here: of the root mean square
+    of all) has steps of 2^-8 of itself or more: at most a sixteenth of them round to
+    another value.  With a dz of 8 bits it would be a quarter."""
+    X, W, t = rows((1, M, D), BF, 461), rows((1, V, D), BF, 462), ids(1, M, V, 463)
+    g = rows((1, M), F32, 464)
+    h = rows((1, M), F32, 465, 0.3) if entropy else None
+    scale = 1 / D ** 0.5
+    _, ent, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=scale)
+    got = tk.tokens_logprobs_grad(X, W, t, lse, g, entropy=ent if entropy else None, grad_entropy=h, scale=scale)
+    want = ref.grads(X, W, t, g, h, scale)
+
+    def off(a, b):
+        large = b.abs() >= (b * b).mean().sqrt()
+        return (a != b.to(BF))[large].double().mean().item()
+    assert off(got[0], want[0]) <= 1 / 16 and off(got[1], want[1]) <= 1 / 16, \
+        (off(got[0], want[0]), off(got[1], want[1]))
+
+
+@pytest.mark.parametrize("M,V,D", [(5_000_000, 40, 264), (6_000_001, 70, 250)])
+def test_table_gradients_of_millions_of_positions(tk, M, V, D):
+    """dW of sums that do not cancel: every position has the same target and gradient, and
+    column d of X the mean 1 + d % 7.  At least 128 shares of M / 128 positions: a running
+    sum is off by at most M / 128 steps of 2^-24 of its magnitude, dz by 2^-11, a result by
+    half a step of bf16, 2^-8.  Left out, one of 256 shares shows in the mean of all."""
+    X = rows((1, M, D), BF, 471, 0.25)
+    X += 1 + torch.arange(D, device="cuda").to(BF) % 7
+    W = rows((1, V, D), BF, 472)
+    t = torch.full((1, M), 3, dtype=torch.int32, device="cuda")
+    g, scale = torch.ones((1, M), device="cuda"), 0.02
+    _, _, lse, _, _ = tk.tokens_logprobs(X, W, t, scale=scale)
+    _, dW = tk.tokens_logprobs_grad(X, W, t, lse, g, scale=scale)
+    want = torch.zeros((V, D), dtype=torch.float64, device="cuda")
+    mag = torch.zeros_like(want)
+    for m in range(0, M, 500_000):
+        x, w = X[0, m:m + 500_000].double(), W[0].double()
+        dz = -torch.softmax(x @ w.t().contiguous() * scale, -1)
+        dz[:, 3] += 1
+        dz = dz.t().contiguous()
+        want += dz @ x * scale
+        mag += dz.abs() @ x.abs() * scale
+    sums = M / 128 * U + H16 + 1e-4  # (1e-4: p's error)
+
+    def right(a):
+        a = a.double()
+        err = (a - want).abs() <= sums * mag + 2.0 ** -8 * (1 + sums) * want.abs()
+        # the roundings' mean over V D results: 2^-8 / sqrt(3 V D), five times that
+        mean = (a / want - 1).mean().abs() <= sums + 5 * 2.0 ** -8 / (3 * V * D) ** 0.5
+        return err.all() and mean
+    assert right(dW[0])
+    assert not right(torch.zeros_like(want)) and not right(want * (1 - 1 / 256)) and not right(want.roll(1, 1))
+
+
 # ---- refusals ---------------------------------------------------------------------------
 def test_refusals_say_what_is_wrong(tk):
     """The library's own status: sizes and numbers that no call takes are invalid, those
