@@ -84,7 +84,7 @@ int tokens_embed_grad(const void* G, int gdtype, const int32_t* idx, int64_t B, 
  * has lse and logprob -inf and entropy 0.  xdtype bf16 or fp16 (fp32 is
  * FKM_ERR_UNSUPPORTED).  A row of X with a NaN has NaN results and no other
  * row has; its top_idx are valid or -1.  D that is no multiple of 8 runs on padded
- * copies.  scale must be finite.  Products scale * <x, w> of magnitude 2^127 and
+ * copies.  scale must be finite.  Products scale * <x, w> of magnitude 2^100 and
  * more are outside the contract; offsets may have any value but NaN and +inf.
  * Workspace: tokens_logprobs_workspace_bytes.
  */

@@ -3,7 +3,8 @@
 Argument marshalling only, as in :mod:`.kmeans`: tensors must be contiguous CUDA
 (HIP) tensors on the current device, work is enqueued on torch's current stream,
 and every output may be passed in.  A table is ``[V, D]`` (one instance) or
-``[B, V, D]``; tokens are int32, and a token outside ``[0, V)`` is none.
+``[B, V, D]``; tokens are int32, and a token outside ``[0, V)`` is none.  The calls take
+no part in autograd: gradients come from the ``_grad`` calls.
 """
 from __future__ import annotations
 
