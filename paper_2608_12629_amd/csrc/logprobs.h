@@ -998,59 +998,78 @@ __device__ __forceinline__ float faint_part(float gs, float top) {
 // value: p = 1 for each of them), a row's maximum and sum are taken again and kept apart.
 constexpr float FAR = 4096.f;
 
-// Both of one row by a workgroup of 512 threads, eight to a table row.  sh: 8 values.
+// Both of up to 16 rows by a workgroup of 512 threads: a wave takes every eighth 16 table
+// rows against all of them in 16 x 16 x 32 MFMAs, fragments straight from memory (x: of
+// the lane's row, lane % 16).  sh: 8 x 16 values; the results in the first 16.  Bound by
+// latency: one row or 16 of 65,536 x 1,024 take their workgroup 4.6 ms, 4,096 of them the
+// call 9.3 ms instead of 2.0 (one row at a time 79).
+constexpr int FAR_R = 16;
 template <int DT>
-__device__ __forceinline__ Stat far_stat(const uint16_t* x, const uint16_t* W, const float* bias,
-                                         float scale, int V, int D, Stat* sh) {
-  const int tid = threadIdx.x, l = tid & 7;
+__device__ __forceinline__ void far_stats(const uint16_t* x, const uint16_t* W, const float* bias,
+                                          float scale, int V, int D, Stat* sh) {
+  constexpr int U = 8;
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), ch = D / 8;
+  const uint4* xc = reinterpret_cast<const uint4*>(x) + q4;
   Stat st = stat_none();
-  for (int v0 = 0; v0 < V; v0 += 64) {
-    const int v = v0 + (tid >> 3);
-    const float bz = v < V ? bias[v] : NEG_INF;
-    float z = 0.f;
-    if (bz != NEG_INF) {
-      const uint4* w = reinterpret_cast<const uint4*>(W + (int64_t)v * D);
-#pragma unroll 4
-      for (int c = l; c < D / 8; c += 8) z = dot_chunk<DT>(reinterpret_cast<const uint4*>(x)[c], w[c], z);
+  for (int v0 = wave * 16; v0 < V; v0 += 128) {
+    const uint4* wc = reinterpret_cast<const uint4*>(W + (int64_t)min(v0 + r16, V - 1) * D) + q4;
+    f32x4 acc = {0, 0, 0, 0};
+    for (int c = 0; c < ch; c += 4 * U) {  // U on their way at a time, zeros past the last
+      uint4 a[U], b[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = c + 4 * u + q4 < ch;
+        a[u] = in ? wc[c + 4 * u] : make_uint4(0, 0, 0, 0);
+        b[u] = in ? xc[c + 4 * u] : make_uint4(0, 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc = mfma_chunk<DT>(a[u], b[u], acc);
     }
 #pragma unroll
-    for (int m = 1; m < 8; m <<= 1) z += __shfl_xor(z, m);
-    if (bz == NEG_INF) continue;
-    z = __builtin_fmaf(z, scale, bz);
-    if (z > st.m) stat_raise(st, z);
-    st.s += __builtin_amdgcn_exp2f((z - st.m) * LOG2E);
+    for (int r = 0; r < 4; ++r) {  // table row v0 + 4 q4 + r, the lane's row
+      const int v = v0 + 4 * q4 + r;
+      const float bz = v < V ? bias[v] : NEG_INF;
+      if (bz == NEG_INF) continue;
+      const float z = __builtin_fmaf(acc[r], scale, bz);
+      if (z > st.m) stat_raise(st, z);
+      st.s += __builtin_amdgcn_exp2f((z - st.m) * LOG2E);
+    }
   }
 #pragma unroll
-  for (int m = 8; m < 64; m <<= 1) {
+  for (int m = 16; m < 64; m <<= 1) {
     const Stat o = {__shfl_xor(st.m, m), __shfl_xor(st.s, m), 0.f};
-    st = stat_merge(tid & m ? o : st, tid & m ? st : o);
+    st = stat_merge(lane & m ? o : st, lane & m ? st : o);
   }
   __syncthreads();
-  if ((tid & 63) == 0) sh[tid >> 6] = st;
+  if (q4 == 0) sh[wave * FAR_R + r16] = st;
   __syncthreads();
-  st = sh[0];
-  for (int i = 1; i < 8; ++i) st = stat_merge(st, sh[i]);
-  return st;
+  if (tid < FAR_R) {
+    for (int i = 1; i < 8; ++i) sh[tid] = stat_merge(sh[tid], sh[i * FAR_R + tid]);
+  }
 }
 
 // What each position's gradient needs, and the largest gs and magnitudes: X's of the
-// rows that take part, W's of the tokens that do.  A workgroup goes over blocks of `rb`
-// rows (about 64 KiB) of X, or past the first `nx` workgroups of W: first a thread per
-// row, then all threads through the rows' 16-byte chunks.
+// rows that take part, W's of the tokens that do.  A workgroup goes over blocks of `rbx`
+// rows (about 64 KiB; with offsets fewer, as far ones may follow) of X, or past the first
+// `nx` workgroups of `rbw` of W: first a thread per row, then all threads through the rows' 16-byte chunks.
 template <int DT, bool BIAS>
 __global__ __launch_bounds__(512) void grad_rows_kernel(
     const uint16_t* __restrict__ X, const uint16_t* __restrict__ W, const int32_t* __restrict__ target,
     const float* __restrict__ lse, const float* __restrict__ ent, const float* __restrict__ g,
     const float* __restrict__ h, const float* __restrict__ bias, float scale, bool exact, int64_t M,
-    int V, int D, int rb, int nx, RowGrad* __restrict__ out, float4* __restrict__ stats) {
+    int V, int D, int rbx, int rbw, int nx, RowGrad* __restrict__ out, float4* __restrict__ stats) {
   __shared__ float sh[8][2];
   __shared__ bool part[512];
   __shared__ float zt_s[DT == DT_F16 ? 512 : 1];
   __shared__ float lse_s[BIAS ? 512 : 1], more_s[BIAS ? 512 : 1];
-  __shared__ Stat far_s[8];
+  __shared__ Stat far_s[BIAS ? 8 * FAR_R : 1];
+  __shared__ int16_t far_q[BIAS ? 512 + FAR_R : 1];
+  __shared__ int far_n;
   const int64_t b = blockIdx.y;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   const bool is_x = (int)blockIdx.x < nx;
+  const int rb = is_x ? rbx : rbw;
   const int64_t rows = is_x ? M : V, nblk = is_x ? nx : gridDim.x - nx;
   const uint16_t* in = (is_x ? X : W) + b * rows * D;
   float gsmax = 0.f;
@@ -1073,10 +1092,21 @@ __global__ __launch_bounds__(512) void grad_rows_kernel(
         part[tid] = far;
       }
       if (__syncthreads_or(far)) {
-        for (int q = 0; q < nr; ++q) {
-          if (!part[q]) continue;
-          const Stat st = far_stat<DT>(in + (r0 + q) * D, W + b * V * D, bias + b * V, scale, V, D, far_s);
-          if (tid == 0) lse_s[q] = st.m, more_s[q] = log2f(st.s);
+        if (tid == 0) {  // the far rows, the last of them once more to a whole group
+          int n = 0;
+          for (int q = 0; q < nr; ++q)
+            if (part[q]) far_q[n++] = q;
+          for (int e = 0; e < FAR_R; ++e) far_q[n + e] = far_q[n - 1];
+          far_n = n;
+        }
+        __syncthreads();
+        for (int i = 0; i < far_n; i += FAR_R) {
+          far_stats<DT>(in + (r0 + far_q[i + (tid & 15)]) * D, W + b * V * D, bias + b * V, scale, V, D,
+                        far_s);
+          if (tid < FAR_R && i + tid < far_n) {
+            lse_s[far_q[i + tid]] = far_s[tid].m;
+            more_s[far_q[i + tid]] = log2f(far_s[tid].s);
+          }
         }
         __syncthreads();
       }
@@ -1966,12 +1996,14 @@ hipError_t launch_grad_dt(const GradArgs& a, const GradWs& w, hipStream_t s) {
   const bool exact = DT == DT_F16 && a.B * a.M <= LP_EXACT;
   const int64_t full = std::max<int64_t>(1, std::min<int64_t>(512, 32768 / w.Dk));
   const int64_t rb = exact ? std::min(full, std::max<int64_t>(16, a.V / 256)) : full;
-  const int64_t nx = std::min<int64_t>((a.M + rb - 1) / rb, STATS_WGS / 2);
+  // with offsets one to a CU, if there are fewer: a far row takes its workgroup a table's worth
+  const int64_t rbx = a.bias ? std::min(rb, std::max<int64_t>(1, a.B * a.M / 256)) : rb;
+  const int64_t nx = std::min<int64_t>((a.M + rbx - 1) / rbx, STATS_WGS / 2);
   const int64_t wgs = nx + std::min<int64_t>((a.V + rb - 1) / rb, STATS_WGS / 2);
   auto grad_rows = a.bias ? grad_rows_kernel<DT, true> : grad_rows_kernel<DT, false>;
   grad_rows<<<dim3((unsigned)wgs, (unsigned)a.B), 512, 0, s>>>(
       (const uint16_t*)X, (const uint16_t*)W, a.target, a.lse, a.entropy, a.g, a.h, a.bias,
-      a.scale, exact, a.M, (int)a.V, (int)w.Dk, (int)rb, (int)nx, w.rows, w.stats);
+      a.scale, exact, a.M, (int)a.V, (int)w.Dk, (int)rbx, (int)rb, (int)nx, w.rows, w.stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   for (int64_t b0 = 0; b0 < a.B; b0 += w.nb) {
     const int64_t nb = std::min<int64_t>(w.nb, a.B - b0);

@@ -119,10 +119,12 @@ def test_gradients_under_offsets_that_all_tokens_share(tk, M, V, D, dt):
     bias[1, V // 2] = LOWEST
     t[1, ::2] = V // 2
     bias[2, 3:] = -2.0 ** 20 - 100
+    W[1, 0], W[2, 1] = INF, float("nan")  # forbidden
     z = ref.scores(X, W, 0.5, None)  # eighths, which stay eighths below 2^21
     z[0] = 0
     z[1], z[1, :, V // 2] = -INF, 0
     z[2, :, :3] = -INF
+    g[:, ::7] = 0
     for h in (None, rows((3, M), F32, 405, 0.3)):
         _, dW = check_sharp(tk, X, W, t, g, h, 0.5, bias, z, torch.zeros_like(z),
                             f"{M, V, D, dt} {h is not None}")
